@@ -162,6 +162,90 @@ int moe_pack_wd(int32_t d_model, int32_t d_ff, int32_t rank, int32_t n_experts, 
 int moe_fp8_quantize_rows(const void* w, int64_t rows, int32_t n, void* codes, float* scales, void* stream);
 int moe_fp8_dequantize_rows(const void* codes, const float* scales, int64_t rows, int32_t n, void* w, void* stream);
 
+/* ---- 4-bit rows (MXFP4) ----------------------------------------------------------
+ * A matrix of `rows` rows of n values in blocks of 32 (the OCP microscaling format): a block has one power of two, a byte s that
+ * stands for 2^(s - 127) (255: NaN), and every value a 4-bit code (sign, two exponent bits, one mantissa bit: 0, .5, 1, 1.5, 2, 3,
+ * 4, 6).  Layout:
+ *    codes   [rows][16 ceil(n / 32)] bytes: value i of a row in byte i / 2, even i in the low four bits; zero behind n
+ *    scales  [ceil(n / 128)][rows rounded up to 4][4] bytes: block b of row r at [b / 4][r][b % 4]; zero behind the last block
+ *            (what rows behind the last one hold is not read)
+ * Experts' matrices lie one after the other: expert e's rows are [e rows / E, (e + 1) rows / E).
+ * moe_fp4_bytes: what codes and scales take.  1 <= n <= MOE_FP4_MAX_N, rows <= MOE_FP4_MAX_ROWS.                       */
+#define MOE_FP4_MAX_N 65536
+#define MOE_FP4_MAX_ROWS (1 << 30)
+typedef struct moe_fp4 {
+  const void* codes;  /* dev, 16-byte aligned                                                                            */
+  const void* scales; /* dev, 16-byte aligned                                                                            */
+  int64_t rows;
+  int32_t n;
+} moe_fp4;
+int moe_fp4_bytes(int64_t rows, int32_t n, size_t* codes_bytes, size_t* scales_bytes);
+/* Row i of the matrix is row r = row_of ? row_of[i] / row_div : i of src (row_of dev [rows], e.g. moe_permute's perm with row_div =
+ * top_k; an r outside [0, src_rows) gives a row of zeros), value c of it at src[r * row_stride + c * col_stride] (dtype MOE_F32 or
+ * MOE_BF16, strides in values, not negative; rows side by side, 16-byte aligned and with n a multiple of 8 are read fastest).
+ * A block's power of two is the largest that is not above its largest magnitude, divided by 4 (at least 2^-127); a code is the
+ * value nearest to v / 2^(s - 127), of two equally near ones the one with the even code, 6 for everything above 5.  A block with
+ * an infinity or a NaN becomes NaN.  rows == 0 is a no-op.                                                              */
+int moe_fp4_quantize_rows(const void* src, int32_t dtype, int64_t src_rows, int64_t row_stride, int64_t col_stride, const int32_t* row_of,
+                          int32_t row_div, int64_t rows, int32_t n, void* codes, void* scales, void* stream);
+/* dst[i * row_stride + c] = the value of row i, column c; exact in either type unless it overflows.  n a multiple of 8, dst 16-byte
+ * aligned, rows of dst a multiple of 16 bytes apart.                                                                    */
+int moe_fp4_dequantize_rows(const moe_fp4* m, void* dst, int32_t dtype, int64_t row_stride, void* stream);
+/* Dense experts (the mathematical layouts of moe_pack_dense) as the two matrices that moe_fp4_experts reads:
+ *    gu    rows E * 64 ceil(f / 32), n = d: per 32 hidden units their 32 gate rows (w_gate[:, c]), then their 32 up rows; rows of
+ *          hidden units behind f are zeros
+ *    down  rows E * d, n = f: w_down[:, j].
+ * The members of gu and down say what is expected and where it goes.                                                   */
+int moe_fp4_pack_dense(int32_t d_model, int32_t d_ff, int32_t n_experts, const void* w_gate, const void* w_up, const void* w_down,
+                       const moe_fp4* gu, const moe_fp4* down, void* stream);
+/* Product of rows grouped by expert with their experts' matrices: for e < E = n_experts, N = w->rows / E,
+ *    out[s * out_stride + j] = sum_i a[s][i] w[e N + j][i]      s in [expert_offsets[e], expert_offsets[e + 1]), j < N
+ * with the values that the codes stand for, fp32 sums, one rounding to out_dtype.  expert_offsets dev [E + 1] int32, ascending, as
+ * moe_permute leaves them; with one expert, the plain product.  Rows of a before the first offset or behind the last are not read
+ * and their rows of out are left as they were.  a->n == w->n, N a multiple of 8, out_stride >= N and a multiple of 8, out 16-byte
+ * aligned, E <= MOE_MAX_EXPERTS.  Above MOE_FP4_FEW_ROWS rows of a on the tensor cores' 4-bit instructions, whose sums of 64
+ * products are cut, not rounded; ctx holds the status word.                                                             */
+#define MOE_FP4_FEW_ROWS 32
+int moe_fp4_product(moe_ctx* ctx, const moe_fp4* a, const moe_fp4* w, const int32_t* expert_offsets, int32_t n_experts, void* out,
+                    int32_t out_dtype, int64_t out_stride, void* stream);
+/* The experts' FFN for a given routing (topk_idx, topk_w dev [T][k], e.g. moe_select's), the experts in MXFP4 (moe_fp4_pack_dense):
+ *    y[t] = sum_j topk_w[t][j] o_tj,   o = h' W_d,  h = silu(x' W_g) * (x' W_u),   x' and h' = x and h rounded to MXFP4
+ * with fp32 sums, h formed in fp32, o in fp32, one rounding of y to cfg.x_dtype.  (h' of a value next to the border between two
+ * codes may fall to either side, as the order of the sums has it.)  x, y dev [T][d].  ctx: of moe_create with wd_rank 0 (path and
+ * renorm are not looked at); an expert index outside [0, E) is reported by moe_check and the output of its token undefined.
+ * ws: moe_fp4_workspace_bytes(cfg, T), enough for fewer tokens too.  Like every call on a ctx, one stream at a time.    */
+int moe_fp4_workspace_bytes(const moe_config* cfg, int32_t T, size_t* bytes);
+int moe_fp4_experts(moe_ctx* ctx, const void* x, int32_t T, const moe_fp4* gu, const moe_fp4* down, const int32_t* topk_idx,
+                    const float* topk_w, void* y, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- expert selection from logits ------------------------------------------------
+ * Per token, l = logits[t * stride + e] (MOE_F32 or MOE_BF16, dev), E = n_experts:
+ *    s_e = softmax(l)_e or 1 / (1 + e^-l_e)                     key_e = s_e + bias[e]  (bias dev [E] fp32 or NULL)
+ *    n_groups > 1: of the groups [g E / G, (g + 1) E / G) those groups_kept whose group_top (1 or 2) largest keys have the largest
+ *    sum; experts of the others are out
+ *    topk_idx[t][j] = the experts with the top_k largest keys, descending;   topk_w[t][j] = scale * s, divided by the sum of the
+ *    chosen s when renorm (0 where that is 0)
+ * Equal keys, and equal groups, go to the lower index.  Keys are formed and compared in 64 bits; where the order of the scores is
+ * that of the logits (no bias, and no sums over groups) the logits are compared.  A logit of -inf switches an expert off: s = 0 and
+ * it comes behind every other one (a token with nothing left gets the lowest experts, with weight 0); NaN counts as -inf; of +inf,
+ * softmax shares 1 among them.  bias must not be NaN.
+ * 1 <= top_k <= MOE_MAX_TOPK, n_experts <= MOE_SELECT_MAX_EXPERTS, n_groups <= 32 and a divisor of n_experts, top_k <= groups_kept
+ * E / G.  No ctx, no workspace; T == 0 is a no-op.                                                                     */
+#define MOE_SELECT_MAX_EXPERTS 256
+enum { MOE_SCORE_SOFTMAX = 0, MOE_SCORE_SIGMOID = 1 };
+typedef struct moe_select_config {
+  int32_t n_experts;
+  int32_t top_k;
+  int32_t scoring;     /* MOE_SCORE_*                                                  */
+  int32_t n_groups;    /* 1: no groups                                                 */
+  int32_t groups_kept;
+  int32_t group_top;   /* keys that a group is judged by: 1 or 2                       */
+  int32_t renorm;      /* 1: a token's weights are rescaled to sum to `scale`          */
+  float scale;
+} moe_select_config;
+int moe_select(const moe_select_config* cfg, const void* logits, int32_t logits_dtype, int64_t stride, int32_t T, const float* bias,
+               int32_t* topk_idx, float* topk_w, void* stream);
+
 /* ---- the layer, step by step ---------------------------------------------------- */
 
 /* Router logits, softmax over experts (Eq. 2), top-k (Eq. 3), gate weights.
@@ -171,6 +255,10 @@ int moe_fp8_dequantize_rows(const void* codes, const float* scales, int64_t rows
  * MOE_STREAM_MAX_TOKENS tokens on the tensor cores, whose sums of eight products are cut, not rounded).  T >= 0 (T == 0 is a no-op).                          */
 int moe_route(moe_ctx* ctx, const void* x, int32_t T, const moe_weights* w, int32_t* topk_idx, float* topk_w,
               float* probs, void* stream);
+
+/* The router's logits alone (b_router, if there is one, added), as moe_route forms them: logits dev [T][E] fp32.  What moe_select
+ * reads.                                                                                                             */
+int moe_route_logits(moe_ctx* ctx, const void* x, int32_t T, const moe_weights* w, float* logits, void* stream);
 
 /* Group the T*k (token, choice) pairs p = t*k + j by expert, stably (token-choice
  * routing gives every expert a discrete set of tokens, Section 2.1).

@@ -4,4 +4,5 @@
 a context and its workspace) that callers and the benchmark use.
 """
 from . import binding  # noqa: F401
-from .layer import MoELayer, OffloadedStack, pack_dense, pack_wd  # noqa: F401
+from .layer import (Fp4Experts, Fp4Rows, MoELayer, OffloadedStack, SelectRule, fp4_product, fp4_quantize,  # noqa: F401
+                    pack_dense, pack_fp4, pack_wd, select_experts)

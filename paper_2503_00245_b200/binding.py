@@ -18,6 +18,9 @@ MOE_OK = 0
 MOE_F32, MOE_BF16 = 0, 1
 MOE_PATH_AUTO, MOE_PATH_STREAM, MOE_PATH_TENSOR = 0, 1, 2
 MOE_STREAM_MAX_TOKENS = 16
+MOE_SCORE_SOFTMAX, MOE_SCORE_SIGMOID = 0, 1
+MOE_SELECT_MAX_EXPERTS = 256
+MOE_FP4_FEW_ROWS = 32
 
 
 class MoeError(RuntimeError):
@@ -31,6 +34,15 @@ class MoeError(RuntimeError):
 class moe_config(C.Structure):
     _fields_ = [(n, C.c_int32) for n in
                 ("d_model", "d_ff", "n_experts", "top_k", "wd_rank", "x_dtype", "renorm", "path")]
+
+
+class moe_fp4(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_int64), ("n", C.c_int32)]
+
+
+class moe_select_config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_experts", "top_k", "scoring", "n_groups", "groups_kept", "group_top", "renorm")] + [
+        ("scale", C.c_float)]
 
 
 class moe_weights(C.Structure):
@@ -54,6 +66,8 @@ _SIGS = {
     "moe_pack_dense": (C.c_int, [C.c_int32] * 3 + [_P] * 5),
     "moe_pack_wd": (C.c_int, [C.c_int32] * 4 + [_P] * 11),
     "moe_route": (C.c_int, [_P, _P, C.c_int32, C.POINTER(moe_weights), _P, _P, _P, _P]),
+    "moe_route_logits": (C.c_int, [_P, _P, C.c_int32, C.POINTER(moe_weights), _P, _P]),
+    "moe_select": (C.c_int, [_P, _P, C.c_int32, C.c_int64, C.c_int32, _P, _P, _P, _P]),
     "moe_permute": (C.c_int, [_P, _P, C.c_int32, _P, _P, _P, _P]),
     "moe_expert_ffn": (C.c_int, [_P, _P, C.c_int32, C.POINTER(moe_weights), _P, _P, _P, _P, C.c_size_t, _P]),
     "moe_combine": (C.c_int, [_P, _P, _P, _P, C.c_int32, _P, _P]),
@@ -66,6 +80,15 @@ _SIGS = {
                                          C.POINTER(_P)]),
     "moe_fp8_quantize_rows": (C.c_int, [_P, C.c_int64, C.c_int32, _P, _P, _P]),
     "moe_fp8_dequantize_rows": (C.c_int, [_P, _P, C.c_int64, C.c_int32, _P, _P]),
+    # (structures as plain addresses, like moe_layer_forward's)
+    "moe_fp4_bytes": (C.c_int, [C.c_int64, C.c_int32, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]),
+    "moe_fp4_quantize_rows": (C.c_int, [_P, C.c_int32, C.c_int64, C.c_int64, C.c_int64, _P, C.c_int32, C.c_int64, C.c_int32, _P, _P,
+                                        _P]),
+    "moe_fp4_dequantize_rows": (C.c_int, [_P, _P, C.c_int32, C.c_int64, _P]),
+    "moe_fp4_pack_dense": (C.c_int, [C.c_int32] * 3 + [_P] * 6),
+    "moe_fp4_product": (C.c_int, [_P, _P, _P, _P, C.c_int32, _P, C.c_int32, C.c_int64, _P]),
+    "moe_fp4_workspace_bytes": (C.c_int, [C.POINTER(moe_config), C.c_int32, C.POINTER(C.c_size_t)]),
+    "moe_fp4_experts": (C.c_int, [_P, _P, C.c_int32, _P, _P, _P, _P, _P, _P, C.c_size_t, _P]),
     "moe_offload_destroy": (C.c_int, [_P]),
     "moe_offload_ensure": (C.c_int, [_P, C.c_int32, C.POINTER(C.c_int32), C.c_int32, _P]),
     "moe_offload_slot_table": (C.c_int, [_P, C.c_int32, C.POINTER(_P)]),
@@ -307,3 +330,80 @@ def moe_fp8_quantize_rows(w, rows, n, codes, scales, stream=None):
 def moe_fp8_dequantize_rows(codes, scales, rows, n, w, stream=None):
     _ok(_lib().moe_fp8_dequantize_rows(_ptr(codes), _ptr(scales), rows, n, _ptr(w), _stream(stream)),
         "moe_fp8_dequantize_rows")
+
+
+def make_select_config(n_experts, top_k, scoring=MOE_SCORE_SOFTMAX, n_groups=1, groups_kept=1, group_top=1, renorm=1, scale=1.0):
+    return moe_select_config(n_experts, top_k, scoring, n_groups, groups_kept, group_top, renorm, scale)
+
+
+def make_fp4(codes, scales, rows, n) -> moe_fp4:
+    m = moe_fp4(_ptr(codes), _ptr(scales), rows, n)
+    m._keep = (codes, scales)
+    return m
+
+
+def _dtype(t) -> int:
+    if t.dtype == torch.float32:
+        return MOE_F32
+    if t.dtype == torch.bfloat16:
+        return MOE_BF16
+    raise TypeError(f"float32 or bfloat16, not {t.dtype}")
+
+
+def moe_route_logits(ctx, x, T, w: moe_weights, logits, stream=None):
+    _ok(_lib().moe_route_logits(ctx, _ptr(x), T, C.byref(w), _ptr(logits), _stream(stream)), "moe_route_logits")
+
+
+def moe_select(cfg: moe_select_config, logits, T, bias, topk_idx, topk_w, stride=None, stream=None):
+    """logits: rows `stride` values apart (n_experts by default), each contiguous."""
+    rc = _lib().moe_select(C.addressof(cfg), logits.data_ptr(), _dtype(logits), cfg.n_experts if stride is None else stride, T,
+                           None if bias is None else _ptr(bias), _ptr(topk_idx), _ptr(topk_w), _stream(stream))
+    if rc:
+        raise MoeError(rc, "moe_select")
+
+
+def moe_fp4_bytes(rows: int, n: int):
+    a, b = C.c_size_t(), C.c_size_t()
+    _ok(_lib().moe_fp4_bytes(rows, n, C.byref(a), C.byref(b)), "moe_fp4_bytes")
+    return a.value, b.value
+
+
+def moe_fp4_quantize_rows(src, row_of, row_div, rows, codes, scales, stream=None):
+    """src [src_rows][n], any strides that are not negative."""
+    rc = _lib().moe_fp4_quantize_rows(src.data_ptr(), _dtype(src), src.shape[0], src.stride(0), src.stride(1),
+                                      None if row_of is None else _ptr(row_of), row_div, rows, src.shape[1], _ptr(codes), _ptr(scales),
+                                      _stream(stream))
+    if rc:
+        raise MoeError(rc, "moe_fp4_quantize_rows")
+
+
+def moe_fp4_dequantize_rows(m: moe_fp4, dst, row_stride=None, stream=None):
+    rc = _lib().moe_fp4_dequantize_rows(C.addressof(m), dst.data_ptr(), _dtype(dst), m.n if row_stride is None else row_stride,
+                                        _stream(stream))
+    if rc:
+        raise MoeError(rc, "moe_fp4_dequantize_rows")
+
+
+def moe_fp4_pack_dense(d, f, n_experts, w_gate, w_up, w_down, gu: moe_fp4, down: moe_fp4, stream=None):
+    _ok(_lib().moe_fp4_pack_dense(d, f, n_experts, _ptr(w_gate), _ptr(w_up), _ptr(w_down), C.addressof(gu), C.addressof(down),
+                                  _stream(stream)), "moe_fp4_pack_dense")
+
+
+def moe_fp4_product(ctx, a: moe_fp4, w: moe_fp4, expert_offsets, n_experts, out, out_stride=None, stream=None):
+    rc = _lib().moe_fp4_product(ctx, C.addressof(a), C.addressof(w), _ptr(expert_offsets), n_experts, out.data_ptr(), _dtype(out),
+                                w.rows // n_experts if out_stride is None else out_stride, _stream(stream))
+    if rc:
+        raise MoeError(rc, "moe_fp4_product")
+
+
+def moe_fp4_workspace_bytes(cfg: moe_config, T: int) -> int:
+    n = C.c_size_t()
+    _ok(_lib().moe_fp4_workspace_bytes(C.byref(cfg), T, C.byref(n)), "moe_fp4_workspace_bytes")
+    return n.value
+
+
+def moe_fp4_experts(ctx, x, T, gu: moe_fp4, down: moe_fp4, topk_idx, topk_w, y, ws, stream=None):
+    rc = _lib().moe_fp4_experts(ctx, _ptr(x), T, C.addressof(gu), C.addressof(down), _ptr(topk_idx), _ptr(topk_w), _ptr(y), _ptr(ws),
+                                ws.nbytes, _stream(stream))
+    if rc:
+        raise MoeError(rc, "moe_fp4_experts")

@@ -240,6 +240,15 @@ int moe_route(moe_ctx* ctx, const void* x, int32_t T, const moe_weights* w, int3
   return launch_route(ctx, x, T, w, topk_idx, topk_w, probs, (cudaStream_t)stream);
 }
 
+int moe_route_logits(moe_ctx* ctx, const void* x, int32_t T, const moe_weights* w, float* logits, void* stream) {
+  if (!ctx || T < 0) return MOE_ERR_INVALID_ARG;
+  if (T == 0) return MOE_OK;
+  if (!x || !logits || misaligned(x)) return MOE_ERR_INVALID_ARG;
+  int rc = check_weights(ctx->cfg, w, true, false);
+  if (rc != MOE_OK) return rc;
+  return launch_route(ctx, x, T, w, nullptr, nullptr, logits, (cudaStream_t)stream);
+}
+
 int moe_permute(moe_ctx* ctx, const int32_t* topk_idx, int32_t T, int32_t* expert_offsets, int32_t* perm,
                 int32_t* inv, void* stream) {
   if (!ctx || T < 0 || !expert_offsets) return MOE_ERR_INVALID_ARG;

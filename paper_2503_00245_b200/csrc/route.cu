@@ -70,6 +70,12 @@ __device__ __forceinline__ void route_partial(const XT* __restrict__ xr, const u
 }
 
 // Many tokens: one warp per token, lanes split the d axis.
+// A launch without topk_idx leaves the logits themselves in `probs`.
+__device__ __forceinline__ void store_logits(float l0, float l1, int E, int lane, float* out) {
+  if (lane < E) out[lane] = l0;
+  if (lane + 32 < E) out[lane + 32] = l1;
+}
+
 template <typename XT, int EMAX>
 __global__ void __launch_bounds__(kRouteWarps * 32)
     route_kernel(const XT* __restrict__ x, const uint16_t* __restrict__ w_router, const float* __restrict__ bias, int T,
@@ -96,6 +102,7 @@ __global__ void __launch_bounds__(kRouteWarps * 32)
   __syncwarp();
   const float l0 = lane < E ? s_logit[wib][lane] + (bias ? bias[lane] : 0.f) : 0.f;
   const float l1 = lane + 32 < E ? s_logit[wib][lane + 32] + (bias ? bias[lane + 32] : 0.f) : 0.f;
+  if (!topk_idx) return store_logits(l0, l1, E, lane, probs + (size_t)t * E);
   warp_route_finish(l0, l1, E, k, renorm, lane, topk_idx + (size_t)t * k, topk_w + (size_t)t * k,
                     probs ? probs + (size_t)t * E : nullptr);
 }
@@ -253,6 +260,7 @@ __global__ void __launch_bounds__(kRtWarps * 32)
       };
       if (lane < E) l0 = logit(lane);
       if (lane + 32 < E) l1 = logit(lane + 32);
+      if (!topk_idx) return store_logits(l0, l1, E, lane, probs + (size_t)t * E);
       int e;
       float wt;
       unsigned long long selected;
@@ -409,6 +417,7 @@ __global__ void __launch_bounds__(kRouteWarps * 32)
     for (int w = 0; w < kRouteWarps; ++w) l1 += s_part[w][lane + 32];
     if (bias) l1 += bias[lane + 32];
   }
+  if (!topk_idx) return store_logits(l0, l1, E, lane, probs + (size_t)t * E);
   warp_route_finish(l0, l1, E, k, renorm, lane, topk_idx + (size_t)t * k, topk_w + (size_t)t * k,
                     probs ? probs + (size_t)t * E : nullptr);
 }

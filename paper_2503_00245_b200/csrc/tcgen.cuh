@@ -149,6 +149,47 @@ __device__ __forceinline__ void tc_wait_ld(uint32_t* a, uint32_t* v) {  // two l
         "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31]));
 }
 
+// 64 bytes of each of 32 rows from a warp's registers (lane = row) to memory, through 2 KB of shared memory: a store of
+// the accumulator layout as it is touches 32 lines with 16 bytes each; this one writes 8 rows' 64 bytes per instruction.
+// (16-byte pieces are swapped by row pair, so that neither side meets a bank conflict.)  rows: valid rows; pieces: valid
+// 16-byte pieces of a row.
+__device__ __forceinline__ void store_rows(unsigned char* buf, int lane, const uint32_t* v, void* dst, long long ld_bytes,
+                                           int rows, int pieces) {
+  __syncwarp();  // (the buffer's last contents have been read)
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    *reinterpret_cast<uint4*>(buf + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4)) =
+        make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+  __syncwarp();
+  const int piece = lane & 3;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = (lane >> 2) + 8 * i;
+    if (r < rows && piece < pieces)
+      *reinterpret_cast<uint4*>((unsigned char*)dst + (long long)r * ld_bytes + piece * 16) =
+          *reinterpret_cast<const uint4*>(buf + r * 64 + ((piece ^ ((r >> 1) & 3)) << 4));
+  }
+}
+// (phone WD r = 128, T = 2048: the layer 163.7 -> 151.2 us; wearable T = 512: 61.6 -> 60.3.)
+// The same for 128 bytes of each row: 4 whole lines per instruction.
+__device__ __forceinline__ void store_rows128(unsigned char* buf, int lane, const uint32_t* v, void* dst, long long ld_bytes,
+                                              int rows, int pieces) {
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    *reinterpret_cast<uint4*>(buf + lane * 128 + ((i ^ (lane & 7)) << 4)) =
+        make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+  __syncwarp();
+  const int piece = lane & 7;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int r = (lane >> 3) + 4 * i;
+    if (r < rows && piece < pieces)
+      *reinterpret_cast<uint4*>((unsigned char*)dst + (long long)r * ld_bytes + piece * 16) =
+          *reinterpret_cast<const uint4*>(buf + r * 128 + ((piece ^ (r & 7)) << 4));
+  }
+}
+
 // Shared-memory operand descriptor (128-byte swizzle).  K-major tiles: rows of 128 bytes, 8-row groups 1024
 // bytes apart (stride byte offset), the leading offset is not used.  N-major tiles: 64 columns (128 bytes) per
 // k-row, 8-k-row groups 1024 bytes apart (stride), 64-column blocks `lbo` bytes apart (leading).

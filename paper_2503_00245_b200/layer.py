@@ -30,12 +30,188 @@ def pack_wd(gL, gR, uL, uR, dL, dR):
     return wd_a, wd_b, wd_c, wd_d
 
 
-class MoELayer:
-    """One MoE layer's packed weights plus a context and workspace sized for up to max_tokens."""
+# ---- 4-bit rows and experts -------------------------------------------------------------
+class Fp4Rows:
+    """A matrix in MXFP4: codes uint8 [rows, 16 ceil(n / 32)] and scales uint8 [ceil(n / 128), rows rounded up to 4, 4] (the layout of
+    moe_fp4 in cosmoe.h)."""
 
-    def __init__(self, d_model, d_ff, n_experts, top_k, w_router, b_router=None, *, dense=None, wd=None,
-                 x_dtype=torch.bfloat16, renorm=True, path=B.MOE_PATH_AUTO, max_tokens=1, expert_slot=None):
-        assert (dense is None) != (wd is None)
+    __slots__ = ("codes", "scales", "rows", "n", "c")
+
+    def __init__(self, codes, scales, n):
+        rows, nb = codes.shape[0], -(-n // 32)
+        if codes.dtype != torch.uint8 or scales.dtype != torch.uint8:
+            raise TypeError("codes and scales are uint8")
+        if tuple(codes.shape) != (rows, 16 * nb) or tuple(scales.shape) != (-(-nb // 4), -(-rows // 4) * 4, 4):
+            raise ValueError(f"codes {tuple(codes.shape)} and scales {tuple(scales.shape)} are not those of {rows} rows of {n} values")
+        if codes.device != scales.device:
+            raise ValueError("codes and scales lie on different devices")
+        self.codes, self.scales, self.rows, self.n = codes, scales, rows, n
+        self.c = B.make_fp4(codes, scales, rows, n)
+
+    @classmethod
+    def empty(cls, rows, n, device="cuda"):
+        nb = -(-n // 32)
+        return cls(torch.empty((rows, 16 * nb), dtype=torch.uint8, device=device),
+                   torch.empty((-(-nb // 4), -(-rows // 4) * 4, 4), dtype=torch.uint8, device=device), n)
+
+    def dequantize(self, dtype=torch.bfloat16):
+        """The values, [rows, n] (n a multiple of 8)."""
+        out = torch.empty((self.rows, self.n), dtype=dtype, device=self.codes.device)
+        _here(self.codes)
+        B.moe_fp4_dequantize_rows(self.c, out)
+        return out
+
+
+def _here(*tensors):
+    """Calls go to the current device's current stream: their tensors have to lie there."""
+    here = B._current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"a tensor on {t.device}, but the current device is cuda:{here}")
+
+
+def fp4_quantize(x, row_of=None, row_div=1):
+    """x [src_rows, n] float32 or bfloat16, any strides -> Fp4Rows; with row_of (int32): row i is x[row_of[i] // row_div]."""
+    if x.dim() != 2:
+        raise ValueError("x is a matrix of rows")
+    rows = x.shape[0]
+    if row_of is not None:
+        if row_of.dtype != torch.int32 or row_of.dim() != 1:
+            raise TypeError("row_of is a vector of int32")
+        rows = row_of.shape[0]
+    _here(x, row_of)
+    q = Fp4Rows.empty(rows, x.shape[1], x.device)
+    B.moe_fp4_quantize_rows(x, row_of, row_div, rows, q.codes, q.scales)
+    return q
+
+
+def pack_fp4(w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor):
+    """[E,d,f], [E,d,f], [E,f,d] bf16 (maths layout) -> the experts in MXFP4: (gu, down)."""
+    E, d, f = w_gate.shape
+    _here(w_gate, w_up, w_down)
+    gu, down = Fp4Rows.empty(E * 64 * -(-f // 32), d, w_gate.device), Fp4Rows.empty(E * d, f, w_gate.device)
+    B.moe_fp4_pack_dense(d, f, E, w_gate, w_up, w_down, gu.c, down.c)
+    return gu, down
+
+
+_shared = {}  # device index -> a ctx for calls that need no more of one than its status word
+
+
+def _shared_ctx():
+    here = B._current_device()
+    if here not in _shared:
+        _shared[here] = B.moe_create(B.make_config(8, 8, 1, 1))
+    return _shared[here]
+
+
+def fp4_product(a: Fp4Rows, w: Fp4Rows, expert_offsets, out=None, out_dtype=torch.bfloat16, ctx=None):
+    """out[s] = a[s] times the matrix of the expert e with expert_offsets[e] <= s < expert_offsets[e + 1]; w holds the experts'
+    matrices, w.rows / E rows each.  Rows outside the offsets are left as they are.  out: rows may lie apart.  Without a ctx (its
+    status word is what moe_check reads) the library's own for this device is used, made by the first call on it."""
+    E = expert_offsets.shape[0] - 1
+    if expert_offsets.dtype != torch.int32 or E < 1:
+        raise TypeError("expert_offsets is a vector of E + 1 int32")
+    N = w.rows // E
+    _here(a.codes, w.codes, expert_offsets, out)
+    if out is None:
+        out = torch.empty((a.rows, N), dtype=out_dtype, device=a.codes.device)
+        stride = N
+    else:
+        if tuple(out.shape) != (a.rows, N) or out.stride(1) != 1:
+            raise ValueError(f"out has to be [{a.rows}, {N}] with contiguous rows")
+        stride = out.stride(0) if a.rows > 1 else max(N, out.stride(0))
+    B.moe_fp4_product(_shared_ctx() if ctx is None else ctx, a.c, w.c, expert_offsets, E, out, stride)
+    return out
+
+
+class SelectRule:
+    """How experts are chosen from logits (moe_select): scoring "softmax" or "sigmoid"; `groups` of which `groups_kept` stay, judged by
+    their `group_top` largest keys; renormalised weights times `scale`."""
+
+    def __init__(self, n_experts, top_k, scoring="softmax", groups=1, groups_kept=1, group_top=1, renorm=True, scale=1.0):
+        self.E, self.k = n_experts, top_k
+        self.c = B.make_select_config(n_experts, top_k, {"softmax": B.MOE_SCORE_SOFTMAX, "sigmoid": B.MOE_SCORE_SIGMOID}[scoring], groups,
+                                      groups_kept, group_top, int(renorm), scale)
+
+
+def select_experts(logits, rule: SelectRule, bias=None):
+    """logits [T, E] float32 or bfloat16 (rows may lie apart), bias [E] float32 -> (topk_idx int32 [T, k], topk_w float32 [T, k])."""
+    if logits.dim() != 2 or logits.shape[1] != rule.E or (rule.E > 1 and logits.stride(1) != 1):
+        raise ValueError(f"logits have to be [T, {rule.E}] with contiguous rows")
+    if bias is not None and (bias.dtype != torch.float32 or bias.shape != (rule.E,)):
+        raise ValueError(f"the bias has to be float32 [{rule.E}]")
+    _here(logits, bias)
+    T = logits.shape[0]
+    idx = torch.empty((T, rule.k), dtype=torch.int32, device=logits.device)
+    w = torch.empty((T, rule.k), dtype=torch.float32, device=logits.device)
+    B.moe_select(rule.c, logits, T, bias, idx, w, logits.stride(0) if T > 1 else rule.E)
+    return idx, w
+
+
+class Fp4Experts:
+    """Experts in MXFP4 (pack_fp4) with a context and a workspace for up to max_tokens: the FFN for a given routing."""
+
+    def __init__(self, d_model, d_ff, n_experts, top_k, gu: Fp4Rows, down: Fp4Rows, x_dtype=torch.bfloat16, max_tokens=1, ctx=None):
+        self.d, self.k, self.x_dtype, self.max_tokens = d_model, top_k, x_dtype, max_tokens
+        self.gu, self.down, self.device = gu, down, gu.codes.device
+        self.cfg = B.make_config(d_model, d_ff, n_experts, top_k, 0, B.MOE_F32 if x_dtype == torch.float32 else B.MOE_BF16)
+        self.ctx, self.lent = ctx, ctx is not None  # (a layer lends its own)
+        _here(gu.codes, down.codes)
+        if ctx is None:
+            self.ctx = B.moe_create(self.cfg)
+        self.ws = torch.empty(B.moe_fp4_workspace_bytes(self.cfg, max_tokens), dtype=torch.uint8, device=self.device)
+
+    def forward(self, x, topk_idx, topk_w, y=None):
+        """x [T, d], topk_idx int32 [T, k], topk_w float32 [T, k] -> y [T, d]."""
+        T = x.shape[0]
+        if T > self.max_tokens:
+            raise ValueError(f"T={T} exceeds max_tokens={self.max_tokens} this workspace was sized for")
+        if x.shape != (T, self.d) or x.dtype != self.x_dtype:
+            raise ValueError(f"x has to be {self.x_dtype} [T, {self.d}]")
+        if topk_idx.shape != (T, self.k) or topk_w.shape != (T, self.k) or topk_idx.dtype != torch.int32 or topk_w.dtype != torch.float32:
+            raise ValueError(f"the routing has to be int32 and float32 [{T}, {self.k}]")
+        _here(x, topk_idx, topk_w, self.ws)
+        if y is None:
+            y = torch.empty((T, self.d), dtype=self.x_dtype, device=self.device)
+        elif y.shape != (T, self.d) or y.dtype != self.x_dtype:
+            raise ValueError(f"y has to be {self.x_dtype} [{T}, {self.d}]")
+        B.moe_fp4_experts(self.ctx, x, T, self.gu.c, self.down.c, topk_idx, topk_w, y, self.ws)
+        return y
+
+    def check(self) -> int:
+        return B.moe_check(self.ctx)
+
+    def close(self):
+        if self.ctx and not self.lent:
+            B.moe_destroy(self.ctx)
+        self.ctx = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class MoELayer:
+    """One MoE layer's packed weights plus a context and workspace sized for up to max_tokens.
+
+    Experts: dense (pack_dense), wd (pack_wd) or fp4 (pack_fp4).  select: a SelectRule that chooses the experts from the router's
+    logits, with select_bias seen by the selection alone, in place of the paper's softmax and top-k."""
+
+    by_steps, select, fp4, ctx = False, None, None, None
+
+    def __init__(self, d_model, d_ff, n_experts, top_k, w_router, b_router=None, *, dense=None, wd=None, fp4=None,
+                 x_dtype=torch.bfloat16, renorm=True, path=B.MOE_PATH_AUTO, max_tokens=1, expert_slot=None, select=None,
+                 select_bias=None):
+        assert (dense is not None) + (wd is not None) + (fp4 is not None) == 1
+        if select is not None and (select.E, select.k) != (n_experts, top_k):
+            raise ValueError("the selection rule is for other numbers of experts")
+        if select is None and select_bias is not None:
+            raise ValueError("select_bias without a selection rule")
+        if fp4 is not None and (path != B.MOE_PATH_AUTO or expert_slot is not None):
+            raise ValueError("4-bit experts take neither a path nor expert_slot")
+        self.select, self.select_bias = select, select_bias
         self.d, self.f, self.E, self.k = d_model, d_ff, n_experts, top_k
         self.x_dtype = x_dtype
         self.device = w_router.device
@@ -45,12 +221,17 @@ class MoELayer:
                                  B.MOE_F32 if x_dtype == torch.float32 else B.MOE_BF16, int(renorm), path)
         if dense is not None:
             self.weights = B.make_weights(w_router, b_router, gud=dense, expert_slot=expert_slot)
-        else:
+        elif wd is not None:
             self.weights = B.make_weights(w_router, b_router, wd_a=wd[0], wd_b=wd[1], wd_c=wd[2], wd_d=wd[3],
                                           expert_slot=expert_slot)
+        else:
+            self.weights = B.make_weights(w_router, b_router)
+        self.by_steps = fp4 is not None or select is not None
         self.ctx = B.moe_create(self.cfg)
         self.max_tokens = max_tokens
-        self.ws = torch.empty(B.moe_workspace_bytes(self.cfg, max_tokens), dtype=torch.uint8, device=self.device)
+        if fp4 is not None:
+            self.fp4 = Fp4Experts(d_model, d_ff, n_experts, top_k, fp4[0], fp4[1], x_dtype, max_tokens, ctx=self.ctx)
+        self.ws = self.fp4.ws if self.fp4 else torch.empty(B.moe_workspace_bytes(self.cfg, max_tokens), dtype=torch.uint8, device=self.device)
 
     @classmethod
     def from_math_layout(cls, shape_kw: dict, tensors: dict, **kw):
@@ -67,8 +248,17 @@ class MoELayer:
             raise ValueError(f"T={T} exceeds max_tokens={self.max_tokens} this layer's workspace was sized for")
 
     # ---- step-by-step calls -------------------------------------------------------------
+    def logits(self, x):
+        out = torch.empty((x.shape[0], self.E), dtype=torch.float32, device=self.device)
+        B.moe_route_logits(self.ctx, x, x.shape[0], self.weights, out)
+        return out
+
     def route(self, x, want_probs=False):
         T = x.shape[0]
+        if self.select is not None:
+            if want_probs:
+                raise ValueError("a selection rule has no probabilities to return")
+            return (*select_experts(self.logits(x), self.select, self.select_bias), None)
         idx = torch.empty((T, self.k), dtype=torch.int32, device=self.device)
         w = torch.empty((T, self.k), dtype=torch.float32, device=self.device)
         probs = torch.empty((T, self.E), dtype=torch.float32, device=self.device) if want_probs else None
@@ -84,6 +274,8 @@ class MoELayer:
         return offsets, perm, inv
 
     def expert_ffn(self, x, offsets, perm):
+        if self.fp4:
+            raise ValueError("4-bit experts: forward, or fp4.forward for a given routing")
         T = x.shape[0]
         self._need(T)
         out = torch.empty((T * self.k, self.d), dtype=torch.float32, device=self.device)
@@ -102,6 +294,8 @@ class MoELayer:
         T = shape[0]
         if T > self.max_tokens:
             self._need(T)
+        if self.by_steps:
+            return self._forward_by_steps(x, y, topk_idx, topk_w)
         if y is None:
             # one token's layer takes about as long as a few calls into PyTorch: y is allocated the cheapest way where that
             # gives the same tensor (a plain one on the layer's device)
@@ -113,10 +307,24 @@ class MoELayer:
         B.moe_layer_forward(self.ctx, x, T, self.weights, y, topk_idx, topk_w, self.ws)
         return y
 
+    def _forward_by_steps(self, x, y, topk_idx, topk_w):
+        idx, w, _ = self.route(x)
+        if topk_idx is not None:
+            topk_idx.copy_(idx)
+        if topk_w is not None:
+            topk_w.copy_(w)
+        if self.fp4:
+            return self.fp4.forward(x, idx, w, y)
+        offsets, perm, inv = self.permute(idx)
+        out = self.combine(self.expert_ffn(x, offsets, perm), w, inv)
+        return out if y is None else y.copy_(out)
+
     def check(self) -> int:
         return B.moe_check(self.ctx)
 
     def close(self):
+        if self.fp4:
+            self.fp4.close()
         if self.ctx:
             B.moe_destroy(self.ctx)
             self.ctx = None
