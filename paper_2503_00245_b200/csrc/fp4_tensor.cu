@@ -6,15 +6,16 @@
 // chip in 17/32 byte a value.
 //
 // A pair of CTAs (cta_group::2) computes tiles of 256 rows x bn <= 192 columns: each CTA stages its 128 rows of A and half of the
-// tile's rows of W, 256 values (128 bytes, one swizzle row) of each at a time.  The scales do not pass through shared memory: four
-// warps fetch a row's word of scales (128 values, csrc/fp4.cuh; 32 neighbouring rows are one line) and store it to tensor memory,
-// where the instruction wants it: word c of lane l is row 32 c + l's, the same in all four quarters of the lanes.  A CTA holds the
-// scales of its own rows and of ALL the tile's columns.  Tensor memory: two accumulators of 192 columns, so that a tile's epilogue
-// runs under the next one's MMAs, and five stages of scales in the 128 columns left.  (bn = 256 would leave room for one accumulator.)
+// tile's rows of W, 256 values (128 bytes, one swizzle row) of each at a time, and the words of scales (128 values each, csrc/fp4.cuh)
+// of its own rows and of ALL the tile's columns.  Four warps carry the words from shared to tensor memory, where the instruction wants
+// them: word c of lane l is row 32 c + l's, the same in all four quarters of the lanes.  Tensor memory: two accumulators of 192
+// columns, so that a tile's epilogue runs under the next one's MMAs, and five stages of scales in the 128 columns left.  (bn = 256
+// would leave room for one accumulator.)
+// (Scales fetched by those warps straight from memory, three stages ahead: 50 us for 4096 rows x 2048 x 5632, 30 without the fetch.)
 // Roles in each CTA:
-//   warp 0      TMA producer: codes of A and W; both CTAs' copies complete on the leader's (rank 0) stage barrier
+//   warp 0      TMA producer: codes of A and W, both CTAs' on the leader's (rank 0) stage barrier; scales, on the CTA's own
 //   warp 1      allocates tensor memory; in the leader one lane issues the MMAs of both CTAs
-//   warps 2-5   scales, memory -> tensor memory (one warp per quarter of the lanes)
+//   warps 2-5   scales, shared -> tensor memory (one warp per quarter of the lanes)
 //   warps 6-13  epilogue
 // Tiles are handed out statically.  A tile may read rows of the next expert, or zeros; they are never stored.  All waits are
 // bounded; one that expires sets the ctx's status word.  No copy here is multicast.
@@ -25,23 +26,26 @@ namespace cosmoe {
 
 namespace {
 
-constexpr int kStages4 = 5;
+constexpr int kStages4 = 6;
 constexpr int kKB = 256;           // values per stage: 128 bytes of codes
 constexpr int kMaxBn = 192;
 constexpr int kScaleWarps = 4;
 constexpr int kThreads4 = (2 + kScaleWarps + kEpiWarps) * 32;
 constexpr int kPairRows4 = 2 * kBM;
-constexpr uint32_t kABytes4 = kBM * 128, kBBytes4 = kMaxBn / 2 * 128, kStageBytes4 = kABytes4 + kBBytes4;
+// A tile's first row is any; a copy starts on 16 bytes, four words of scales: up to three rows before the first come along.
+constexpr int kScaleRowsA = kBM + 4;
+constexpr uint32_t kABytes4 = kBM * 128, kWBytes4 = kMaxBn / 2 * 128;
+constexpr uint32_t kSABytes4 = 2 * kScaleRowsA * 4, kSAOff4 = kABytes4 + kWBytes4, kSWOff4 = kSAOff4 + (kSABytes4 + 127) / 128 * 128;
+constexpr uint32_t kStageBytes4 = (kSWOff4 + 2 * kMaxBn * 4 + 1023) / 1024 * 1024;
 constexpr int kScaleCol = 2 * kMaxBn;   // first column of the scales; a stage: A 4 + 4, W 8 + 8 columns
 constexpr int kScaleCols = 24;
-static_assert(kScaleCol + kStages4 * kScaleCols <= kTmemCols, "tensor memory");
+constexpr int kScaleSlots = 5;
+static_assert(kScaleCol + kScaleSlots * kScaleCols <= kTmemCols && kScaleSlots < kStages4, "tensor memory");
 constexpr int kEpiBuf4 = 4096;
 
 enum { EPI4_F32 = 0, EPI4_BF16 = 1, EPI4_HIDDEN = 2 };
 
 struct Fp4Params {
-  const uint32_t *a_scales, *w_scales;
-  Fp4Shape a, w;
   int n_rows;              // of A
   const int32_t* offsets;  // [E + 1]
   int E, N, K;
@@ -54,10 +58,12 @@ struct Fp4Params {
 };
 
 struct Smem4 {
-  uint64_t full[kStages4];   // leader's: the codes of the stage have landed in both CTAs, and both CTAs' scales are in place
-  uint64_t empty[kStages4];  // own: the MMAs have finished with this CTA's stage
-  uint64_t accum_full[2];    // own
-  uint64_t accum_empty[2];   // leader's
+  uint64_t full[kStages4];       // leader's: the codes of the stage have landed in both CTAs
+  uint64_t scales_in[kStages4];  // own: its words of scales have landed
+  uint64_t scales_at[kStages4];  // leader's: both CTAs' scales are in tensor memory
+  uint64_t empty[kStages4];      // own: the MMAs have finished with this CTA's stage
+  uint64_t accum_full[2];        // own
+  uint64_t accum_empty[2];       // leader's
   uint32_t tmem_base;
 };
 
@@ -129,33 +135,9 @@ __device__ __forceinline__ void tc_st2(uint32_t taddr, const uint32_t* v) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x2.b32 [%0], {%1, %2};" ::"r"(taddr), "r"(v[0]), "r"(v[1]) : "memory");
 }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void arrive_release_cluster(uint32_t bar_cluster) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster) : "memory");
-}
-// (the scales of the other CTA are announced from there)
-__device__ __forceinline__ bool wait_acquire_cluster(uint64_t* bar, uint32_t parity) {
-  auto ready = [&] {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity)
-        : "memory");
-    return ok != 0;
-  };
-  bool got = ready();
-  if (!got) {
-    const long long t0 = clock64();
-    while (!(got = ready()))
-      if (clock64() - t0 > kWaitBudgetCycles) break;
-  }
-  return __all_sync(0xffffffffu, got);
-}
-
 __global__ void __launch_bounds__(kThreads4, 1)
-    fp4_tensor_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_w, const Fp4Params P) {
+    fp4_tensor_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_w,
+                      const __grid_constant__ CUtensorMap map_sa, const __grid_constant__ CUtensorMap map_sw, const Fp4Params P) {
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   unsigned char* stages = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   unsigned char* const epi_bufs = stages + (size_t)kStages4 * kStageBytes4;
@@ -168,7 +150,9 @@ __global__ void __launch_bounds__(kThreads4, 1)
 
   if (tid == 0) {
     for (int i = 0; i < kStages4; ++i) {
-      mbar_init(&sm.full[i], 1 + 2 * kScaleWarps);
+      mbar_init(&sm.full[i], 1);
+      mbar_init(&sm.scales_in[i], 1);
+      mbar_init(&sm.scales_at[i], 2 * kScaleWarps);
       mbar_init(&sm.empty[i], 1);
     }
     for (int b = 0; b < 2; ++b) {
@@ -203,6 +187,7 @@ __global__ void __launch_bounds__(kThreads4, 1)
     bool ok = true;
     const uint32_t tx_pair = 2u * (kABytes4 + (uint32_t)P.bn / 2u * 128u);
     const uint32_t full0 = (uint32_t)lane0((int)map_to_rank(&sm.full[0], 0u));
+    const uint32_t own0 = (uint32_t)lane0((int)map_to_rank(&sm.scales_in[0], rank));
     const uint32_t st0 = (uint32_t)lane0((int)smem_u32(stages));
     for (int idx = pair; ok && idx < n_work; idx += n_pairs) {
       const Tile4 t = tile_at(P, tm, idx, n_tiles);
@@ -213,8 +198,11 @@ __global__ void __launch_bounds__(kThreads4, 1)
           ok = false;
           break;
         }
-        const uint32_t st_a = st0 + slot * kStageBytes4, bar = full0 + 8u * slot;
+        const uint32_t st_a = st0 + slot * kStageBytes4, bar = full0 + 8u * slot, own = own0 + 8u * slot;
         if (elect_one()) {
+          mbar_arrive_expect_tx(&sm.scales_in[slot], kSABytes4 + (uint32_t)P.bn * 8u);
+          tma_load_2d(st_a + kSAOff4, &map_sa, a_row & ~3, 2 * kb, own);
+          tma_load_2d(st_a + kSWOff4, &map_sw, t.e * P.N + t.n0, 2 * kb, own);
           if (rank == 0) mbar_arrive_expect_tx(&sm.full[slot], tx_pair);
           tma_load_2d(st_a, &map_a, kb * 128, a_row, bar);
           tma_load_2d(st_a + kABytes4, &map_w, kb * 128, w_row, bar);
@@ -223,8 +211,11 @@ __global__ void __launch_bounds__(kThreads4, 1)
         if (++slot == (uint32_t)kStages4) slot = 0, par ^= 1u;
       }
     }
-    if (!ok && rank == 0) {  // copies in flight must land before the pair goes away
-      for (int j = max(0, it - kStages4); j < it; ++j) (void)mbar_wait(&sm.full[j % kStages4], (j / kStages4) & 1);
+    if (!ok) {  // copies in flight must land before the pair goes away
+      for (int j = max(0, it - kStages4); j < it; ++j) {
+        (void)mbar_wait(&sm.scales_in[j % kStages4], (j / kStages4) & 1);
+        if (rank == 0) (void)mbar_wait(&sm.full[j % kStages4], (j / kStages4) & 1);
+      }
     }
   } else if (warp == 1) {
     // ================================================================= MMA issuer (leader only)
@@ -232,7 +223,7 @@ __global__ void __launch_bounds__(kThreads4, 1)
       const uint32_t id0 = instr_desc_mxf4(P.bn, 0u), id2 = instr_desc_mxf4(P.bn, 2u);
       const uint64_t hi_k = smem_desc(0, 16, 1024) & 0xffffffff00000000ull;
       const uint32_t stage0 = (uint32_t)lane0((int)(smem_u32(stages) >> 4));
-      uint32_t slot = 0, par = 0, st_lo = stage0;
+      uint32_t slot = 0, par = 0, st_lo = stage0, sc_slot = 0;
       int tile_i = 0;
       bool ok = true;
       for (int idx = pair; ok && idx < n_work; idx += n_pairs, ++tile_i) {
@@ -246,7 +237,7 @@ __global__ void __launch_bounds__(kThreads4, 1)
         }
         const uint32_t d_tmem = tmem + (uint32_t)(buf * kMaxBn);
         for (int kb = 0; kb < num_kb; ++kb) {
-          if (!wait_acquire_cluster(&sm.full[slot], par)) {
+          if (!mbar_wait_warp(&sm.full[slot], par) || !mbar_wait_warp(&sm.scales_at[slot], par)) {
             if (lane == 0) flag_error(P.st, MOE_ERR_TIMEOUT, 0x601u);
             ok = false;
             break;
@@ -254,7 +245,7 @@ __global__ void __launch_bounds__(kThreads4, 1)
           tc_fence_after();
           const uint64_t da = hi_k | (uint64_t)(st_lo | (1u << 16));
           const uint64_t db = hi_k | (uint64_t)((st_lo + (kABytes4 >> 4)) | (1u << 16));
-          const uint32_t sc = tmem + (uint32_t)kScaleCol + slot * (uint32_t)kScaleCols;
+          const uint32_t sc = tmem + (uint32_t)kScaleCol + sc_slot * (uint32_t)kScaleCols;
           const int steps = min(4, (P.K - kb * kKB + 63) / 64);
           if (elect_one()) {
 #pragma unroll
@@ -267,6 +258,7 @@ __global__ void __launch_bounds__(kThreads4, 1)
           }
           __syncwarp();
           st_lo += kStageBytes4 >> 4;
+          if (++sc_slot == (uint32_t)kScaleSlots) sc_slot = 0;
           if (++slot == (uint32_t)kStages4) slot = 0, par ^= 1u, st_lo = stage0;
         }
       }
@@ -274,75 +266,50 @@ __global__ void __launch_bounds__(kThreads4, 1)
   } else if (warp < 2 + kScaleWarps) {
     // ================================================================= scales (both CTAs)
     const uint32_t quarter = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + (uint32_t)kScaleCol;
-    const uint32_t full0 = (uint32_t)lane0((int)map_to_rank(&sm.full[0], 0u));
-    constexpr int kAhead = 3;  // stages whose words are on their way
-    uint32_t v[kAhead][20];
-    const int nc = P.bn / 32;
-    // the stage after the last one asked for
-    int f_idx = pair, f_kb = 0;
-    const uint32_t* f_a[4];
-    const uint32_t* f_w[6];
-    auto enter = [&] {
-      if (f_idx >= n_work) return;
-      const Tile4 t = tile_at(P, tm, f_idx, n_tiles);
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int r = t.m0 + (int)rank * kBM + 32 * c + lane;
-        f_a[c] = r < P.n_rows ? P.a_scales + r : nullptr;
-      }
-#pragma unroll
-      for (int c = 0; c < 6; ++c) {
-        const int r = t.n0 + 32 * c + lane;
-        f_w[c] = c < nc && r < P.N ? P.w_scales + (long long)t.e * P.N + r : nullptr;
-      }
-    };
-    auto fetch = [&](uint32_t* o) {
-      if (f_idx >= n_work) return;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const long long ch = 2 * f_kb + h;
-        const bool in = ch < P.a.chunks;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) o[10 * h + c] = in && f_a[c] ? __ldcg(f_a[c] + ch * P.a.rp) : 0u;
-#pragma unroll
-        for (int c = 0; c < 6; ++c) o[10 * h + 4 + c] = in && f_w[c] ? __ldg(f_w[c] + ch * P.w.rp) : 0u;
-      }
-      if (++f_kb == num_kb) {
-        f_kb = 0, f_idx += n_pairs;
-        enter();
-      }
-    };
-    enter();
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) fetch(v[i]);
-    const long long n_stages = n_work > pair ? (long long)((n_work - pair + n_pairs - 1) / n_pairs) * num_kb : 0;
-    uint32_t slot = 0, par = 1;
+    const uint32_t at0 = (uint32_t)lane0((int)map_to_rank(&sm.scales_at[0], 0u));
+    uint32_t slot = 0, par = 0, sc_slot = 0;
+    int it = 0, e_slot = 0, e_par = 0;  // (the stage whose MMAs must be done with the tensor memory written next)
     bool ok = true;
-    for (long long it0 = 0; ok && it0 < n_stages; it0 += kAhead) {
+    for (int idx = pair; ok && idx < n_work; idx += n_pairs) {
+      const Tile4 t = tile_at(P, tm, idx, n_tiles);
+      const int skip = (t.m0 + (int)rank * kBM) & 3;
+      for (int kb = 0; kb < num_kb; ++kb, ++it) {
+        if (!mbar_wait_warp(&sm.scales_in[slot], par)) {
+          if (lane == 0) flag_error(P.st, MOE_ERR_TIMEOUT, 0x605u);
+          ok = false;
+          break;
+        }
+        const uint32_t* sa = reinterpret_cast<const uint32_t*>(stages + slot * kStageBytes4 + kSAOff4) + skip + lane;
+        const uint32_t* sw = reinterpret_cast<const uint32_t*>(stages + slot * kStageBytes4 + kSWOff4) + lane;
+        uint32_t v[2][10];
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const long long it = it0 + i;
-        if (it >= n_stages) break;
-        if (it >= kStages4) {
-          if (!mbar_wait_warp(&sm.empty[slot], par)) {
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) v[h][c] = sa[h * kScaleRowsA + 32 * c];
+#pragma unroll
+          for (int c = 0; c < 6; ++c) v[h][4 + c] = 32 * c < P.bn ? sw[h * P.bn + 32 * c] : 0u;
+        }
+        if (it >= kScaleSlots) {
+          if (!mbar_wait_warp(&sm.empty[e_slot], e_par)) {
             if (lane == 0) flag_error(P.st, MOE_ERR_TIMEOUT, 0x604u);
             ok = false;
             break;
           }
           tc_fence_after();
+          if (++e_slot == kStages4) e_slot = 0, e_par ^= 1;
         }
-        const uint32_t at = quarter + slot * (uint32_t)kScaleCols;
+        const uint32_t at = quarter + sc_slot * (uint32_t)kScaleCols;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          tc_st4(at + 4u * h, v[i] + 10 * h);
-          tc_st4(at + 8u + 8u * h, v[i] + 10 * h + 4);
-          tc_st2(at + 12u + 8u * h, v[i] + 10 * h + 8);
+          tc_st4(at + 4u * h, v[h]);
+          tc_st4(at + 8u + 8u * h, v[h] + 4);
+          tc_st2(at + 12u + 8u * h, v[h] + 8);
         }
         tc_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) arrive_release_cluster(full0 + 8u * slot);
-        fetch(v[i]);
+        if (lane == 0) mbar_arrive_cluster(at0 + 8u * slot);
+        if (++sc_slot == (uint32_t)kScaleSlots) sc_slot = 0;
         if (++slot == (uint32_t)kStages4) slot = 0, par ^= 1u;
       }
     }
@@ -436,22 +403,36 @@ int make_map_codes(CUtensorMap* m, const void* base, long long rows, long long p
   return r == CUDA_SUCCESS ? MOE_OK : MOE_ERR_CUDA;
 }
 
+// words of scales [chunks][rp]: box of box_rows words x 2
+int make_map_scales(CUtensorMap* m, const void* base, const Fp4Shape& sh, int box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return MOE_ERR_CUDA;
+  const cuuint64_t dims[2] = {(cuuint64_t)sh.rp, (cuuint64_t)sh.chunks};
+  const cuuint64_t strides[1] = {(cuuint64_t)sh.rp * 4};
+  const cuuint32_t box[2] = {(cuuint32_t)box_rows, 2};
+  const cuuint32_t es[2] = {1, 1};
+  const CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? MOE_OK : MOE_ERR_CUDA;
+}
+
 }  // namespace
 
 // out_f32: 1 fp32, 0 bf16; h (not null): hidden rows instead of `out`.
 int launch_fp4_tensor(moe_ctx* ctx, const moe_fp4* a, const moe_fp4* w, const int32_t* offsets, int E, void* out, int out_f32,
                       long long out_stride, const moe_fp4* h, cudaStream_t s) {
   Fp4Params P{};
-  P.a = fp4_shape(a->rows, a->n), P.w = fp4_shape(w->rows, w->n);
-  P.a_scales = (const uint32_t*)a->scales, P.w_scales = (const uint32_t*)w->scales;
+  const Fp4Shape sa = fp4_shape(a->rows, a->n), sw = fp4_shape(w->rows, w->n);
   P.n_rows = (int)a->rows, P.offsets = offsets, P.E = E, P.N = (int)(w->rows / E), P.K = a->n;
   P.out = out, P.ld_out = out_stride, P.epi = h ? EPI4_HIDDEN : out_f32 ? EPI4_F32 : EPI4_BF16;
   if (h) P.h_codes = (unsigned char*)h->codes, P.h_scales = (unsigned char*)h->scales, P.h = fp4_shape(h->rows, h->n);
   P.st = ctx->d_state;
   P.bn = P.N > 128 ? kMaxBn : P.N > 64 ? 128 : 64;
-  CUtensorMap ma, mw;
-  MOE_TRY(make_map_codes(&ma, a->codes, a->rows, P.a.pitch, kBM));
-  MOE_TRY(make_map_codes(&mw, w->codes, w->rows, P.w.pitch, P.bn / 2));
+  CUtensorMap ma, mw, msa, msw;
+  MOE_TRY(make_map_codes(&ma, a->codes, a->rows, sa.pitch, kBM));
+  MOE_TRY(make_map_codes(&mw, w->codes, w->rows, sw.pitch, P.bn / 2));
+  MOE_TRY(make_map_scales(&msa, a->scales, sa, kScaleRowsA));
+  MOE_TRY(make_map_scales(&msw, w->scales, sw, P.bn));
   const size_t smem = (size_t)kStages4 * kStageBytes4 + kEpiWarps * kEpiBuf4 + sizeof(Smem4) + 1024 + 128;
   if ((long long)smem > ctx->max_smem_optin) return MOE_ERR_UNSUPPORTED;
   MOE_TRY(allow_full_smem<fp4_tensor_kernel>(ctx));
@@ -461,7 +442,7 @@ int launch_fp4_tensor(moe_ctx* ctx, const moe_fp4* a, const moe_fp4* w, const in
   cudaLaunchConfig_t lc;
   cudaLaunchAttribute attr[2];
   pair_launch_config(lc, attr, 2 * pairs, kThreads4, smem, s);
-  MOE_CUDA_TRY(cudaLaunchKernelEx(&lc, fp4_tensor_kernel, ma, mw, P));
+  MOE_CUDA_TRY(cudaLaunchKernelEx(&lc, fp4_tensor_kernel, ma, mw, msa, msw, P));
   ctx->launches++;
   return MOE_OK;
 }
