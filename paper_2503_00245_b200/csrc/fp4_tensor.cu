@@ -29,8 +29,8 @@ namespace {
 constexpr int kStages4 = 6;
 constexpr int kKB = 256;           // values per stage: 128 bytes of codes
 constexpr int kMaxBn = 192;
-constexpr int kScaleWarps = 4;
-constexpr int kThreads4 = (2 + kScaleWarps + kEpiWarps) * 32;
+constexpr int kScaleWarps = 4, kScaleSets = 2;
+constexpr int kThreads4 = (2 + kScaleSets * kScaleWarps + kEpiWarps) * 32;
 constexpr int kPairRows4 = 2 * kBM;
 // A tile's first row is any; a copy starts on 16 bytes, four words of scales: up to three rows before the first come along.
 constexpr int kScaleRowsA = kBM + 4;
@@ -263,24 +263,30 @@ __global__ void __launch_bounds__(kThreads4, 1)
         }
       }
     }
-  } else if (warp < 2 + kScaleWarps) {
+  } else if (warp < 2 + kScaleSets * kScaleWarps) {
     // ================================================================= scales (both CTAs)
     const uint32_t quarter = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + (uint32_t)kScaleCol;
     const uint32_t at0 = (uint32_t)lane0((int)map_to_rank(&sm.scales_at[0], 0u));
     uint32_t slot = 0, par = 0, sc_slot = 0;
+    const int set = (warp - 2) / kScaleWarps;
     int it = 0, e_slot = 0, e_par = 0;  // (the stage whose MMAs must be done with the tensor memory written next)
     bool ok = true;
     for (int idx = pair; ok && idx < n_work; idx += n_pairs) {
       const Tile4 t = tile_at(P, tm, idx, n_tiles);
       const int skip = (t.m0 + (int)rank * kBM) & 3;
       for (int kb = 0; kb < num_kb; ++kb, ++it) {
-        if (!mbar_wait_warp(&sm.scales_in[slot], par)) {
+        const uint32_t this_slot = slot, this_par = par, this_sc = sc_slot, this_e = e_slot, this_epar = e_par;
+        if (++sc_slot == (uint32_t)kScaleSlots) sc_slot = 0;
+        if (++slot == (uint32_t)kStages4) slot = 0, par ^= 1u;
+        if (it >= kScaleSlots && ++e_slot == kStages4) e_slot = 0, e_par ^= 1;
+        if (it % kScaleSets != set) continue;
+        if (!mbar_wait_warp(&sm.scales_in[this_slot], this_par)) {
           if (lane == 0) flag_error(P.st, MOE_ERR_TIMEOUT, 0x605u);
           ok = false;
           break;
         }
-        const uint32_t* sa = reinterpret_cast<const uint32_t*>(stages + slot * kStageBytes4 + kSAOff4) + skip + lane;
-        const uint32_t* sw = reinterpret_cast<const uint32_t*>(stages + slot * kStageBytes4 + kSWOff4) + lane;
+        const uint32_t* sa = reinterpret_cast<const uint32_t*>(stages + this_slot * kStageBytes4 + kSAOff4) + skip + lane;
+        const uint32_t* sw = reinterpret_cast<const uint32_t*>(stages + this_slot * kStageBytes4 + kSWOff4) + lane;
         uint32_t v[2][10];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -290,15 +296,14 @@ __global__ void __launch_bounds__(kThreads4, 1)
           for (int c = 0; c < 6; ++c) v[h][4 + c] = 32 * c < P.bn ? sw[h * P.bn + 32 * c] : 0u;
         }
         if (it >= kScaleSlots) {
-          if (!mbar_wait_warp(&sm.empty[e_slot], e_par)) {
+          if (!mbar_wait_warp(&sm.empty[this_e], this_epar)) {
             if (lane == 0) flag_error(P.st, MOE_ERR_TIMEOUT, 0x604u);
             ok = false;
             break;
           }
           tc_fence_after();
-          if (++e_slot == kStages4) e_slot = 0, e_par ^= 1;
         }
-        const uint32_t at = quarter + sc_slot * (uint32_t)kScaleCols;
+        const uint32_t at = quarter + this_sc * (uint32_t)kScaleCols;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           tc_st4(at + 4u * h, v[h]);
@@ -308,14 +313,12 @@ __global__ void __launch_bounds__(kThreads4, 1)
         tc_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(at0 + 8u * slot);
-        if (++sc_slot == (uint32_t)kScaleSlots) sc_slot = 0;
-        if (++slot == (uint32_t)kStages4) slot = 0, par ^= 1u;
+        if (lane == 0) mbar_arrive_cluster(at0 + 8u * this_slot);
       }
     }
   } else {
     // ================================================================= epilogue (warps 6..13, both CTAs)
-    const int ew = warp - (2 + kScaleWarps);
+    const int ew = warp - (2 + kScaleSets * kScaleWarps);
     const int q = warp & 3;
     const uint32_t acce_bar[2] = {map_to_rank(&sm.accum_empty[0], 0u), map_to_rank(&sm.accum_empty[1], 0u)};
     unsigned char* const ebuf = epi_bufs + ew * kEpiBuf4;
@@ -360,19 +363,22 @@ __global__ void __launch_bounds__(kThreads4, 1)
             }
           }
         } else {
-          for (int c = 32 * cpar; c < ncols; c += 64) {
-            uint32_t a[32];
-            tc_ld32(tbase + c, a);
-            tc_wait_ld(a);
+          for (int c = 64 * cpar; c < ncols; c += 128) {
+            uint32_t a[2][32];
+            tc_ld32(tbase + c, a[0]);
+            tc_ld32(tbase + c + 32, a[1]);
+            tc_wait_ld(a[0], a[1]);
             if (P.epi == EPI4_F32) {
-              store_rows128(ebuf, lane, a, (float*)P.out + (long long)(row - lane) * P.ld_out + t.n0 + c, P.ld_out * 4, rows,
-                            (ncols - c) / 4);
+              float* const o = (float*)P.out + (long long)(row - lane) * P.ld_out + t.n0 + c;
+              store_rows128(ebuf, lane, a[0], o, P.ld_out * 4, rows, (ncols - c) / 4);
+              store_rows128(ebuf, lane, a[1], o + 32, P.ld_out * 4, rows, (ncols - c) / 4 - 8);
             } else {
-              uint32_t o[16];
+              uint32_t o[32];
 #pragma unroll
-              for (int j = 0; j < 16; ++j) o[j] = pack_bf16x2(__uint_as_float(a[2 * j]), __uint_as_float(a[2 * j + 1]));
-              store_rows(ebuf, lane, o, (__nv_bfloat16*)P.out + (long long)(row - lane) * P.ld_out + t.n0 + c, P.ld_out * 2, rows,
-                         (ncols - c) / 8);
+              for (int j = 0; j < 32; ++j)
+                o[j] = pack_bf16x2(__uint_as_float(a[j >> 4][2 * (j & 15)]), __uint_as_float(a[j >> 4][2 * (j & 15) + 1]));
+              store_rows128(ebuf, lane, o, (__nv_bfloat16*)P.out + (long long)(row - lane) * P.ld_out + t.n0 + c, P.ld_out * 2, rows,
+                            (ncols - c) / 8);
             }
           }
         }
