@@ -65,8 +65,8 @@ struct moe_ctx {
   long long* acc;                // device: fixed-point output accumulators of the dense streaming path, kept zero
   size_t acc_elems;              //         between calls by the kernel itself (MOE_STREAM_MAX_TOKENS*top_k*d)
   unsigned long long launches;
-  std::atomic<unsigned>* smem_ok;  // kernels that may use all the shared memory of a CTA, a bit each (allow_full_smem)
-  std::atomic<unsigned> smem_ok_own;
+  std::atomic<unsigned long long>* smem_ok;  // kernels that may use all the shared memory of a CTA, a bit each (allow_full_smem)
+  std::atomic<unsigned long long> smem_ok_own;
   long long fin_wait_budget;     // cycles the dense streaming kernel's finalisers wait for the arrival counter (0 = default)
 };
 
@@ -76,13 +76,13 @@ namespace cosmoe {
 // front of every launch.  (The limit only permits; a launch still takes what it asks for.  It is an attribute of the function
 // in one CUDA context, as a ctx's memory belongs to one: a device may have several.)
 constexpr int kMaxDevices = 64;
-inline unsigned next_smem_bit() {
+inline unsigned long long next_smem_bit() {  // (at most 64 kernels ask)
   static std::atomic<unsigned> n{0};
-  return 1u << n.fetch_add(1);
+  return 1ull << n.fetch_add(1);
 }
 template <auto Kernel>
 int allow_full_smem(const moe_ctx* ctx) {
-  static const unsigned bit = next_smem_bit();
+  static const unsigned long long bit = next_smem_bit();
   if (ctx->smem_ok->load(std::memory_order_relaxed) & bit) return MOE_OK;
   cudaFuncAttributes fa{};
   MOE_CUDA_TRY(cudaFuncGetAttributes(&fa, Kernel));

@@ -1613,7 +1613,7 @@ struct StaticDevice {
   int rc;               // outcome of the one-off set-up
   unsigned char* base;  // device address of g_static_scratch on this GPU
   int sm_count, max_smem_optin;
-  std::atomic<unsigned> smem_ok;  // as of a ctx: the array's address belongs to one CUDA context as well
+  std::atomic<unsigned long long> smem_ok;  // as of a ctx: the array's address belongs to one CUDA context as well
 };
 StaticDevice g_static_dev[kMaxDevices];
 

@@ -78,4 +78,15 @@ struct Fp4Source {
 // Destination rows: i, or, with `split` 0 or 1, row i of a matrix whose blocks of 32 rows alternate with another's.
 int launch_fp4_quantize(const Fp4Source& src, long long rows, int n, void* codes, void* scales, long long rp, int split, cudaStream_t s);
 
+// csrc/fp4_few.cu: few rows (decode)
+constexpr int kFewSplits = 4;  // parts of the down product's contraction, at most
+bool fp4_few_applies(const moe_ctx* ctx, int K, int n);  // (n: rows of an expert, at most, without an expert named twice by a token)
+int launch_fp4_few_rows(moe_ctx* ctx, const moe_fp4* a, const moe_fp4* w, const int32_t* offsets, int E, void* out, int out_f32,
+                        long long out_stride, cudaStream_t s);
+int launch_fp4_few_experts(moe_ctx* ctx, const void* x, int T, const moe_fp4* gu, const moe_fp4* down, const int32_t* idx, const float* wt,
+                           void* y, const moe_fp4* h, float* part, unsigned* arrived, cudaStream_t s);
+// csrc/fp4_tensor.cu: many rows.  out_f32: 1 fp32, 0 bf16; h (not null): hidden rows of MXFP4 instead of `out`.
+int launch_fp4_tensor(moe_ctx* ctx, const moe_fp4* a, const moe_fp4* w, const int32_t* offsets, int E, void* out, int out_f32,
+                      long long out_stride, const moe_fp4* h, cudaStream_t s);
+
 }  // namespace cosmoe

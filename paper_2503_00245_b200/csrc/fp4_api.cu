@@ -5,13 +5,6 @@
 
 namespace cosmoe {
 
-int launch_fp4_rows(moe_ctx* ctx, const moe_fp4* a, const moe_fp4* w, const int32_t* idx, const int32_t* offsets, int E, void* out,
-                    int out_f32, long long out_stride, cudaStream_t s);
-int launch_fp4_few(moe_ctx* ctx, const void* x, int T, const moe_fp4* gu, const moe_fp4* down, const int32_t* idx, const float* wt, void* y,
-                   const moe_fp4* h, float* out_slots, cudaStream_t s);
-int launch_fp4_tensor(moe_ctx* ctx, const moe_fp4* a, const moe_fp4* w, const int32_t* offsets, int E, void* out, int out_f32,
-                      long long out_stride, const moe_fp4* h, cudaStream_t s);
-
 namespace {
 
 bool misaligned(const void* p) { return ((uintptr_t)p & 15u) != 0; }
@@ -25,7 +18,7 @@ int check_matrix(const moe_fp4* m) {
 // Scratch of moe_fp4_experts.
 struct Fp4Ws {
   size_t offsets, perm, inv;
-  size_t x_codes, x_scales, h_codes, h_scales, out_slots, total;
+  size_t x_codes, x_scales, h_codes, h_scales, out_slots, arrived, total;
 };
 Fp4Ws fp4_ws(const moe_config& c, int T) {
   Fp4Ws L{};
@@ -41,7 +34,10 @@ Fp4Ws fp4_ws(const moe_config& c, int T) {
   L.perm = take((size_t)n * 4), L.inv = take((size_t)n * 4);
   L.x_codes = take((size_t)n * x.pitch), L.x_scales = take((size_t)x.chunks * x.rp * 4);
   L.h_codes = take((size_t)n * h.pitch), L.h_scales = take((size_t)h.chunks * h.rp * 4);
-  L.out_slots = take((size_t)n * c.d_model * 4);
+  // (few tokens: planes of the down product's parts)
+  const long long few = (long long)std::min(T, MOE_STREAM_MAX_TOKENS) * c.top_k * kFewSplits;
+  L.out_slots = take((size_t)std::max(n, few) * c.d_model * 4);
+  L.arrived = take((size_t)((c.d_model + 63) / 64) * 4);
   L.total = off;
   return L;
 }
@@ -67,8 +63,8 @@ int moe_fp4_product(moe_ctx* ctx, const moe_fp4* a, const moe_fp4* w, const int3
   if (a->rows == 0) return MOE_OK;
   if (!expert_offsets || !out || misaligned(out) || ((uintptr_t)expert_offsets & 3u)) return MOE_ERR_INVALID_ARG;
   cudaStream_t s = (cudaStream_t)stream;
-  if (a->rows <= MOE_FP4_FEW_ROWS)
-    return launch_fp4_rows(ctx, a, w, nullptr, expert_offsets, n_experts, out, out_dtype == MOE_F32, out_stride, s);
+  if (a->rows <= MOE_FP4_FEW_ROWS && fp4_few_applies(ctx, a->n, (int)a->rows))
+    return launch_fp4_few_rows(ctx, a, w, expert_offsets, n_experts, out, out_dtype == MOE_F32, out_stride, s);
   return launch_fp4_tensor(ctx, a, w, expert_offsets, n_experts, out, out_dtype == MOE_F32, out_stride, nullptr, s);
 }
 
@@ -104,7 +100,8 @@ int moe_fp4_experts(moe_ctx* ctx, const void* x, int32_t T, const moe_fp4* gu, c
   const int n = T * c.top_k;
   const moe_fp4 xq{b + L.x_codes, b + L.x_scales, n, c.d_model}, h{b + L.h_codes, b + L.h_scales, n, c.d_ff};
   float* const o = (float*)(b + L.out_slots);
-  if (T <= MOE_STREAM_MAX_TOKENS) return launch_fp4_few(ctx, x, T, gu, down, topk_idx, topk_w, y, &h, o, s);
+  if (T <= MOE_STREAM_MAX_TOKENS && fp4_few_applies(ctx, c.d_model, T) && fp4_few_applies(ctx, c.d_ff, T))
+    return launch_fp4_few_experts(ctx, x, T, gu, down, topk_idx, topk_w, y, &h, o, (unsigned*)(b + L.arrived), s);
   int32_t *offsets = (int32_t*)(b + L.offsets), *perm = (int32_t*)(b + L.perm), *inv = (int32_t*)(b + L.inv);
   rc = launch_permute(ctx, topk_idx, T, offsets, perm, inv, s);
   if (rc != MOE_OK) return rc;
