@@ -8,7 +8,7 @@
 // instruction costs its operands' 4 KB of shared-memory reads either way), the tokens N = 16 or 32 columns, whose codes are laid out
 // in shared memory, swizzled.  Both operands' scales go from shared to tensor memory beside the MMAs (two sets of four warps, a stage
 // each in turn).
-//   warp 0       copies (the ring's first fill: with warps 1, 10 and 11)
+//   warp 0       copies (the ring's first fill: a stage for each warp)
 //   warp 1       tensor memory, MMAs
 //   warps 2-9    scales                     warps 12-13  epilogue (TMEM lanes 0-31 and 32-63)
 // Most of this code runs once or twice a launch, so it is short rather than unrolled: fetching instructions that were never run costs
@@ -36,7 +36,7 @@ constexpr int kFewStages = 12, kFewSlots = 6;
 // tensor memory: two accumulators of 32 columns, scales of six stages, matrix and tokens (four columns for 128 values each)
 constexpr int kSlotCol = 64, kSlotCols = 32, kFewTmem = 256;
 static_assert(kSlotCol + kFewSlots * kSlotCols <= kFewTmem, "tensor memory");
-constexpr int kSets = 2, kFillWarps = 4;
+constexpr int kSets = 2;
 constexpr int kFewLast = 256;  // (d_model is at most 16384)
 
 enum { FEW_HIDDEN = 0, FEW_OUT = 1, FEW_DOWN = 2 };
@@ -53,6 +53,7 @@ struct FewParams {
   const int32_t *idx, *offsets;  // one of the two: whose rows are whose
   int n, E;
   int units, splits, stages, m;  // blocks of an expert; parts of the contraction; ring; columns of an MMA
+  int part_stages;               // of the contraction's parts (the last one may be shorter)
   void* out;
   long long out_stride;
   int out_f32;
@@ -79,10 +80,12 @@ struct FewSmem {
   float acc[2][32][kBlkRows];  // the epilogue's accumulators, [token][row], two blocks in turn
 };
 
-__device__ __forceinline__ void few_load(uint32_t dst, const CUtensorMap* map, int c0, int c1, uint64_t* bar) {
+// (Read once: first to leave L2, so that what the next product will read stays there.)
+__device__ __forceinline__ void few_load(uint32_t dst, const CUtensorMap* map, int c0, int c1, uint64_t* bar, uint64_t policy) {
   asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map),
-      "r"(c0), "r"(c1), "r"(smem_u32(bar))
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;" ::
+          "r"(dst),
+      "l"(map), "r"(c0), "r"(c1), "r"(smem_u32(bar)), "l"(policy)
       : "memory");
 }
 __device__ __forceinline__ void few_commit(uint64_t* bar) {
@@ -211,44 +214,80 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   const int groups = mine > 0 ? (cnt + P.m - 1) / P.m : 0;
   auto item_of = [&](int i, int& unit, int& sp, int& s0, int& s1) {
     const int item = rank + i * ctas;
-    unit = item / P.splits, sp = item - unit * P.splits;
-    s0 = sp * all_stages / P.splits, s1 = (sp + 1) * all_stages / P.splits;
+    unit = P.splits == 1 ? item : item / P.splits, sp = item - unit * P.splits;
+    s0 = sp * P.part_stages, s1 = min(s0 + P.part_stages, all_stages);
   };
   const uint32_t st0 = smem_u32(stages);
 
-  // ---- copies, in (group, item, stage) order
-  int c_it = 0, c_i = 0, c_s = 0, c_g = 0;
-  bool copies_ok = true;
-  // By a whole warp, for stages of group g before the most-th: those that are `which` modulo `of` are its own.
-  auto copy_until = [&](int most, int g, int which, int of) {
-    while (copies_ok && c_g == g && c_it < most) {
-      int unit, sp, s0, s1;
-      item_of(c_i, unit, sp, s0, s1);
-      const int b = c_it % NS, s = s0 + c_s;
-      if (c_it % of == which) {
-        if (c_it >= NS && !mbar_wait_warp(&sm.empty[b], (c_it / NS - 1) & 1)) {
-          if (lane == 0) flag_error(P.st, MOE_ERR_TIMEOUT, 0x510u);
-          copies_ok = false;
-          break;
-        }
-        if (elect_one()) {
-          const uint32_t at = st0 + (uint32_t)b * kFewStage;
-          const int row = e * P.N + unit * kBlkRows;
-          mbar_arrive_expect_tx(&sm.full[b], kFewStage);
-          few_load(at, &map_w, s * 256, row, &sm.full[b]);
-          few_load(at + kHalfBytes, &map_w, s * 256 + 128, row, &sm.full[b]);
-          few_load(at + 2 * kHalfBytes, &map_s, row, 4 * s, &sm.full[b]);
-        }
-        __syncwarp();
+  // ---- the tokens' codes and scales.  A warp takes 256 values of a token at a time; the next ones' loads are on their way meanwhile.
+  // (The first of them go out in front of the matrix's copies: behind 25 MB of those they take 3 us.)
+  int tok = 0, step = 0;  // (of 256 values)
+  uint4 u = make_uint4(0u, 0u, 0u, 0u), v = u;
+  uint32_t word = 0u, s_word = 0u;
+  auto fetch = [&](int g0) {
+    const int c = step * 256 + lane * 8;
+    const long long r = sm.rows[g0 + tok];
+    if (MODE == FEW_HIDDEN) {
+      const long long at = r / P.k * P.K + min(c, P.K - 8);
+      if (P.x_f32) {
+        u = __ldcg(reinterpret_cast<const uint4*>((const float*)P.x + at));
+        v = __ldcg(reinterpret_cast<const uint4*>((const float*)P.x + at) + 1);
+      } else {
+        u = __ldcg(reinterpret_cast<const uint4*>((const __nv_bfloat16*)P.x + at));
       }
-      ++c_it;
-      if (++c_s == s1 - s0) {
-        c_s = 0;
-        if (++c_i == mine) c_i = 0, ++c_g;
-      }
+    } else {
+      word = c < 32 * P.a.nb ? __ldcg(reinterpret_cast<const uint32_t*>(P.a_codes + r * P.a.pitch + (c >> 1))) : 0u;
+      s_word = (lane & 15) == 0 && c < P.K ? __ldcg(P.a_scales + (c >> 7) * P.a.rp + r) : 0u;
     }
   };
-  if (groups > 0 && (warp < 2 || warp == 10 || warp == 11)) copy_until(NS, 0, warp & 3, kFillWarps);  // (0, 1, 2 and 3)
+  auto first_fetch = [&](int g0, int have) {
+    tok = 0, step = warp;
+    while (step >= steps && tok < have) step -= steps, ++tok;
+    if (tok < have) fetch(g0);
+  };
+  if (MODE != FEW_DOWN && groups > 0) first_fetch(0, min(P.m, cnt));
+
+  // ---- copies, in (group, item, stage) order.  The ring's first fill is a stage for each warp, all at once: what a single warp
+  // does one after the other here takes a tenth of a microsecond a copy.
+  const uint64_t once = l2_policy_evict_first();
+  auto copy = [&](int b, int unit, int s) {  // by one lane
+    const uint32_t at = st0 + (uint32_t)b * kFewStage;
+    const int row = e * P.N + unit * kBlkRows;
+    mbar_arrive_expect_tx(&sm.full[b], kFewStage);
+    few_load(at, &map_w, s * 256, row, &sm.full[b], once);
+    few_load(at + kHalfBytes, &map_w, s * 256 + 128, row, &sm.full[b], once);
+    few_load(at + 2 * kHalfBytes, &map_s, row, 4 * s, &sm.full[b], once);
+  };
+  int c_i = 0, c_s = 0, c_it = 0;         // item and stage of the next copy, and its number
+  int c_left = warp == 0 ? NS : warp;     // (stages to walk on to it)
+  if (groups > 0) {
+    auto walk = [&] {  // c_left stages on; stops behind the last item
+      while (c_i < mine) {
+        int unit, sp, s0, s1;
+        item_of(c_i, unit, sp, s0, s1);
+        if (c_left < s1 - s0) {
+          c_s = s0 + c_left;
+          return true;
+        }
+        c_left -= s1 - s0, ++c_i;
+      }
+      return false;
+    };
+    if (warp < NS) {
+      int unit, sp, s0, s1;
+      if (warp == 0) {
+        item_of(0, unit, sp, s0, s1);
+        if (elect_one()) copy(0, unit, s0);
+        __syncwarp();
+        c_it = walk() ? NS : NS - c_left;
+      } else if (walk()) {
+        item_of(c_i, unit, sp, s0, s1);
+        if (elect_one()) copy(warp, unit, c_s);
+        __syncwarp();
+      }
+    }
+  }
+  bool copies_ok = true;
   if (MODE == FEW_DOWN) {
     pdl_wait();
     pdl_launch_dependents();
@@ -268,51 +307,67 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   bool ok = true;
   for (int g0 = 0, grp = 0; grp < groups; g0 += P.m, ++grp) {
     const int have = min(P.m, cnt - g0);
-    // ---- the tokens' codes and scales.  Four lanes per block of 32; columns behind the last token stay as they are.
-    const int quads = chunks * 16 * have;
-    for (int i = tid; i < quads; i += kFewThreads) {
-      const unsigned all = i - lane + 32 <= quads ? 0xffffffffu : 0xffffu;  // (sixteen lanes to a word of scales)
-      const int q = i & 3, b = (i >> 2) & 3, rest = i >> 4, ch = rest % chunks, tok = rest / chunks;
-      const int c = ch * 128 + b * 32 + q * 8;  // first of eight values
-      uint32_t word = 0u, s = 0u;
-      const long long r = sm.rows[g0 + tok];
-      if (MODE == FEW_HIDDEN) {
-        float f[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = 0.f;
-        if (c < P.K) {
-          const long long at = r / P.k * P.K + c;
+    // (four lanes to a block of 32; columns behind the last token stay as they are)
+    {
+      const int q = lane & 3, b = (lane >> 2) & 3;
+      if (grp > 0 || MODE == FEW_DOWN) first_fetch(g0, have);
+#pragma unroll 1
+      while (tok < have) {
+        const int my_tok = tok, my_step = step, c = step * 256 + lane * 8;
+        const uint4 mu = u, mv = v;
+        uint32_t w = word, sc = s_word;
+        step += kFewThreads / 32;
+        while (step >= steps && tok < have) step -= steps, ++tok;
+        if (tok < have) fetch(g0);
+        if (MODE == FEW_HIDDEN) {
+          float f[8];
           if (P.x_f32) {
-            const float4* src = reinterpret_cast<const float4*>((const float*)P.x + at);
-            const float4 u = __ldcg(src), v = __ldcg(src + 1);
-            f[0] = u.x, f[1] = u.y, f[2] = u.z, f[3] = u.w, f[4] = v.x, f[5] = v.y, f[6] = v.z, f[7] = v.w;
+            const float4 a = *reinterpret_cast<const float4*>(&mu), d = *reinterpret_cast<const float4*>(&mv);
+            f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = d.x, f[5] = d.y, f[6] = d.z, f[7] = d.w;
           } else {
-            unpack8(__ldcg(reinterpret_cast<const uint4*>((const __nv_bfloat16*)P.x + at)), f);
+            unpack8(mu, f);
           }
-        }
-        uint32_t top = 0u;
+          uint32_t top = 0u;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(f[j]) & 0x7fffffffu);
-        top = max(top, __shfl_xor_sync(all, top, 1));
-        top = max(top, __shfl_xor_sync(all, top, 2));
-        s = fp4_scale_byte(top);
-        word = fp4_pack8(f, fp4_up(s));
-        uint32_t w = s << (8 * b);
-        w |= __shfl_xor_sync(all, w, 4);
-        w |= __shfl_xor_sync(all, w, 8);
-        if ((i & 15) == 0) tok_scales[ch * P.m + tok] = w;
-      } else {
-        if (4 * ch + b < P.a.nb) word = __ldcg(reinterpret_cast<const uint32_t*>(P.a_codes + r * P.a.pitch + (c >> 1)));
-        if ((i & 15) == 0) tok_scales[ch * P.m + tok] = __ldcg(P.a_scales + ch * P.a.rp + r);
+          for (int j = 0; j < 8; ++j) {
+            if (c >= P.K) f[j] = 0.f;
+            top = max(top, __float_as_uint(f[j]) & 0x7fffffffu);
+          }
+          top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+          const uint32_t byte = fp4_scale_byte(top);
+          w = fp4_pack8(f, fp4_up(byte));
+          sc = byte << (8 * b);
+          sc |= __shfl_xor_sync(0xffffffffu, sc, 4);
+          sc |= __shfl_xor_sync(0xffffffffu, sc, 8);
+        }
+        if (q + b == 0 && (c >> 7) < chunks) tok_scales[(c >> 7) * P.m + my_tok] = sc;
+        *reinterpret_cast<uint32_t*>(toks + (size_t)my_step * (P.m * 128) + my_tok * 128 + (((lane >> 2) ^ (my_tok & 7)) << 4) + q * 4) = w;
       }
-      const int byte = (c & 255) >> 1;
-      *reinterpret_cast<uint32_t*>(toks + (size_t)(c >> 8) * (P.m * 128) + tok * 128 + (((byte >> 4) ^ (tok & 7)) << 4) + (byte & 15)) = word;
     }
     fence_proxy_async_smem();
     __syncthreads();
 
     if (warp == 0) {
-      copy_until(0x7fffffff, grp, 0, 1);
+      // ------------------------------------------------------------- copies
+      int b = c_it % NS, round = c_it / NS;
+      if (grp > 0) c_i = 0, c_s = -1;
+      while (copies_ok && c_i < mine) {
+        int unit, sp, s0, s1;
+        item_of(c_i, unit, sp, s0, s1);
+        if (c_s < 0) c_s = s0;
+        for (; c_s < s1; ++c_s, ++c_it) {
+          if (round > 0 && !mbar_wait_warp(&sm.empty[b], (round - 1) & 1)) {
+            if (lane == 0) flag_error(P.st, MOE_ERR_TIMEOUT, 0x510u);
+            copies_ok = false;
+            break;
+          }
+          if (elect_one()) copy(b, unit, c_s);
+          __syncwarp();
+          if (++b == NS) b = 0, ++round;
+        }
+        ++c_i, c_s = -1;
+      }
     } else if (warp == 1) {
       // ------------------------------------------------------------- MMAs
       const uint32_t id0 = few_idesc(P.m, 0u), id2 = few_idesc(P.m, 2u);
@@ -450,8 +505,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
             else ((__nv_bfloat16*)P.out)[sm.rows[g0 + t] * P.out_stride + r] = __float2bfloat16_rn(v);
           }
         }
-        if (MODE == FEW_DOWN) {
-          __threadfence();
+        if (MODE == FEW_DOWN) {  // (released by one thread behind the barrier)
           epilogue_meet();
           if (warp == 12 && lane == 0 && atom_add_acq_rel(P.arrived + unit, 1u) == (unsigned)sm.expected - 1u) sm.last_unit[sm.n_last++] = unit;
         }
@@ -534,6 +588,8 @@ int few_launch(moe_ctx* ctx, const moe_fp4* w, FewParams& P, const FewPlan& plan
   CUtensorMap codes, scales;
   MOE_TRY(few_maps(w, &codes, &scales));
   P.K = w->n, P.w = fp4_shape(w->rows, w->n), P.N = (int)(w->rows / P.E);
+  const int all = (P.K + kStageK - 1) / kStageK;
+  P.part_stages = (all + P.splits - 1) / P.splits, P.splits = (all + P.part_stages - 1) / P.part_stages;
   P.units = (P.N + kBlkRows - 1) / kBlkRows, P.stages = plan.stages, P.m = plan.m, P.st = ctx->d_state;
   MOE_TRY((allow_full_smem<fp4_few_kernel<MODE>>(ctx)));
   const int most = std::min(P.E, P.n);  // experts with rows
@@ -583,9 +639,9 @@ int launch_fp4_few_experts(moe_ctx* ctx, const void* x, int T, const moe_fp4* gu
   FewParams D{};
   D.a_codes = (const unsigned char*)h->codes, D.a_scales = (const uint32_t*)h->scales, D.a = P.h;
   D.idx = idx, D.n = n, D.E = E, D.k = c.top_k, D.T = T, D.wt = wt, D.y = y, D.y_f32 = P.x_f32, D.part = part, D.arrived = arrived;
-  // parts of the contraction: about two for each SM
+  // parts of the contraction where blocks alone leave SMs idle
   const int units = (c.d_model + kBlkRows - 1) / kBlkRows, all = (c.d_ff + kStageK - 1) / kStageK;
-  D.splits = std::max(1, std::min({kFewSplits, all, 2 * ctx->sm_count / (units * most)}));
+  D.splits = std::max(1, std::min({kFewSplits, all, ctx->sm_count / (units * most)}));
   return few_launch<FEW_DOWN>(ctx, down, D, plan, s);
 }
 
