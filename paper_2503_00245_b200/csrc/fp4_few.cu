@@ -53,6 +53,7 @@ struct FewParams {
   const int32_t *idx, *offsets;  // one of the two: whose rows are whose
   int n, E;
   int units, splits, stages, m;  // blocks of an expert; parts of the contraction; ring; columns of an MMA
+  int tok_rows;                  // rows of tokens in shared memory: m, or 8 where 16 columns show the same eight twice
   int part_stages;               // of the contraction's parts (the last one may be shorter)
   void* out;
   long long out_stride;
@@ -76,8 +77,7 @@ struct FewSmem {
   uint32_t tmem_base;
   int e, cnt, rank, ctas, expected, n_last;
   int rows[kFewRows];
-  int last_unit[kFewLast];     // DOWN: blocks whose last part came from here
-  float acc[2][32][kBlkRows];  // the epilogue's accumulators, [token][row], two blocks in turn
+  int last_unit[kFewLast];  // DOWN: blocks whose last part came from here
 };
 
 // (Read once: first to leave L2, so that what the next product will read stays there.)
@@ -163,7 +163,7 @@ __device__ __forceinline__ void few_find(const FewParams& P, FewSmem& sm, int la
           have += __popc(is);
         }
         if (ee == e) cnt = have;
-        expected += (have + P.m - 1) / P.m;
+        expected += (have + P.tok_rows - 1) / P.tok_rows;
       }
     } else {
       const int lo = max(P.offsets[e], 0);
@@ -175,17 +175,19 @@ __device__ __forceinline__ void few_find(const FewParams& P, FewSmem& sm, int la
 }
 
 template <int MODE>
-__global__ void __launch_bounds__(kFewThreads, 1)
+__global__ void __launch_bounds__(kFewThreads, 2)
     fp4_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_s, const FewParams P) {
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   __shared__ FewSmem sm;
   unsigned char* const stages = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   const int tid = threadIdx.x, lane = tid & 31, warp = lane0(tid >> 5);
   const int NS = P.stages, slots = min(NS, kFewSlots);
-  // tokens: codes [256 values][m rows][128 bytes], words of scales [chunk][m]
+  // tokens: codes [256 values][tok_rows][128 bytes], words of scales [chunk][tok_rows]; behind them the epilogue's accumulators,
+  // [token][row], two blocks in turn
   const int chunks = P.w.chunks, steps = (chunks + 1) / 2;
   unsigned char* const toks = stages + (((size_t)NS * kFewStage + 1023) & ~(size_t)1023);
-  uint32_t* const tok_scales = reinterpret_cast<uint32_t*>(toks + (size_t)steps * P.m * 128);
+  uint32_t* const tok_scales = reinterpret_cast<uint32_t*>(toks + (size_t)steps * P.tok_rows * 128);
+  float* const accs = reinterpret_cast<float*>(tok_scales + (size_t)chunks * P.tok_rows);
 
   if (tid == 0) {
     for (int i = 0; i < NS; ++i) mbar_init(&sm.full[i], 1), mbar_init(&sm.scales_at[i], 4), mbar_init(&sm.empty[i], 1);
@@ -211,7 +213,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   const int items = e >= 0 ? P.units * P.splits : 0;
   const int mine = rank < items ? (items - rank + ctas - 1) / ctas : 0;
   const int all_stages = (P.K + kStageK - 1) / kStageK;
-  const int groups = mine > 0 ? (cnt + P.m - 1) / P.m : 0;
+  const int groups = mine > 0 ? (cnt + P.tok_rows - 1) / P.tok_rows : 0;
   auto item_of = [&](int i, int& unit, int& sp, int& s0, int& s1) {
     const int item = rank + i * ctas;
     unit = P.splits == 1 ? item : item / P.splits, sp = item - unit * P.splits;
@@ -226,9 +228,9 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   uint32_t word = 0u, s_word = 0u;
   auto fetch = [&](int g0) {
     const int c = step * 256 + lane * 8;
-    const long long r = sm.rows[g0 + tok];
+    const int r = sm.rows[g0 + tok];
     if (MODE == FEW_HIDDEN) {
-      const long long at = r / P.k * P.K + min(c, P.K - 8);
+      const long long at = (long long)(r / P.k) * P.K + min(c, P.K - 8);
       if (P.x_f32) {
         u = __ldcg(reinterpret_cast<const uint4*>((const float*)P.x + at));
         v = __ldcg(reinterpret_cast<const uint4*>((const float*)P.x + at) + 1);
@@ -245,7 +247,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
     while (step >= steps && tok < have) step -= steps, ++tok;
     if (tok < have) fetch(g0);
   };
-  if (MODE != FEW_DOWN && groups > 0) first_fetch(0, min(P.m, cnt));
+  if (MODE != FEW_DOWN && groups > 0) first_fetch(0, min(P.tok_rows, cnt));
 
   // ---- copies, in (group, item, stage) order.  The ring's first fill is a stage for each warp, all at once: what a single warp
   // does one after the other here takes a tenth of a microsecond a copy.
@@ -305,8 +307,8 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   uint32_t slot = 0, par = 0, sc_slot = 0;          // MMA and scale warps: places in the rings
   int it = 0, e_slot = 0, e_par = 0, acc_i = 0;     // stages so far; the stage that frees the scale slot; accumulators so far
   bool ok = true;
-  for (int g0 = 0, grp = 0; grp < groups; g0 += P.m, ++grp) {
-    const int have = min(P.m, cnt - g0);
+  for (int g0 = 0, grp = 0; grp < groups; g0 += P.tok_rows, ++grp) {
+    const int have = min(P.tok_rows, cnt - g0);
     // (four lanes to a block of 32; columns behind the last token stay as they are)
     {
       const int q = lane & 3, b = (lane >> 2) & 3;
@@ -341,8 +343,8 @@ __global__ void __launch_bounds__(kFewThreads, 1)
           sc |= __shfl_xor_sync(0xffffffffu, sc, 4);
           sc |= __shfl_xor_sync(0xffffffffu, sc, 8);
         }
-        if (q + b == 0 && (c >> 7) < chunks) tok_scales[(c >> 7) * P.m + my_tok] = sc;
-        *reinterpret_cast<uint32_t*>(toks + (size_t)my_step * (P.m * 128) + my_tok * 128 + (((lane >> 2) ^ (my_tok & 7)) << 4) + q * 4) = w;
+        if (q + b == 0 && (c >> 7) < chunks) tok_scales[(c >> 7) * P.tok_rows + my_tok] = sc;
+        *reinterpret_cast<uint32_t*>(toks + (size_t)my_step * (P.tok_rows * 128) + my_tok * 128 + (((lane >> 2) ^ (my_tok & 7)) << 4) + q * 4) = w;
       }
     }
     fence_proxy_async_smem();
@@ -372,6 +374,8 @@ __global__ void __launch_bounds__(kFewThreads, 1)
       // ------------------------------------------------------------- MMAs
       const uint32_t id0 = few_idesc(P.m, 0u), id2 = few_idesc(P.m, 2u);
       const uint64_t hi_k = smem_desc(0, 16, 1024) & 0xffffffff00000000ull;
+      // (eight rows of tokens: the second group of eight columns reads them again)
+      const uint64_t hi_tok = smem_desc(0, 16, P.tok_rows == 8 ? 0 : 1024) & 0xffffffff00000000ull;
       const uint32_t tok_lo = (uint32_t)lane0((int)(smem_u32(toks) >> 4)), ring_lo = st0 >> 4;
       for (int i = 0; ok && i < mine; ++i, ++acc_i) {
         int unit, sp, s0, s1;
@@ -393,14 +397,14 @@ __global__ void __launch_bounds__(kFewThreads, 1)
           }
           tc_fence_after();
           const int mmas = min(8, (P.K - s * kStageK + 63) / 64);
-          const uint32_t a_lo = ring_lo + slot * (kFewStage >> 4), b_lo = tok_lo + (uint32_t)(2 * s) * (uint32_t)(P.m * 8);
+          const uint32_t a_lo = ring_lo + slot * (kFewStage >> 4), b_lo = tok_lo + (uint32_t)(2 * s) * (uint32_t)(P.tok_rows * 8);
           const uint32_t sa = tmem + (uint32_t)kSlotCol + (uint32_t)kSlotCols * sc_slot, sb = sa + 16u;
           if (elect_one()) {
 #pragma unroll
             for (uint32_t j = 0; j < 8; ++j)
               if ((int)j < mmas) {
                 const uint64_t da = hi_k | (uint64_t)((a_lo + (j >> 2) * (kHalfBytes >> 4) + 2u * (j & 3u)) | (1u << 16));
-                const uint64_t db = hi_k | (uint64_t)((b_lo + (j >> 2) * (uint32_t)(P.m * 8) + 2u * (j & 3u)) | (1u << 16));
+                const uint64_t db = hi_tok | (uint64_t)((b_lo + (j >> 2) * (uint32_t)(P.tok_rows * 8) + 2u * (j & 3u)) | (1u << 16));
                 few_mma(tmem + 32u * buf, da, db, (j & 1u) ? id2 : id0, sa + 4u * (j >> 1), sb + 4u * (j >> 1), (uint32_t)(s - s0) | j);
               }
             few_commit(&sm.empty[slot]);
@@ -425,6 +429,16 @@ __global__ void __launch_bounds__(kFewThreads, 1)
           if (++slot == (uint32_t)NS) slot = 0, par ^= 1u;
           if (it >= slots && ++e_slot == NS) e_slot = 0, e_par ^= 1;
           if (it % kSets != set) continue;
+          // (First the stage whose place in tensor memory this one takes: a set sees every other stage only, and with that one done
+          // the phase of `full` before this one's is over, without which the wait below would not wait.)
+          if (it >= slots) {
+            if (!mbar_wait_warp(&sm.empty[this_e], this_epar)) {
+              if (lane == 0) flag_error(P.st, MOE_ERR_TIMEOUT, 0x514u);
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+          }
           if (!mbar_wait_warp(&sm.full[this_slot], this_par)) {
             if (lane == 0) flag_error(P.st, MOE_ERR_TIMEOUT, 0x513u);
             ok = false;
@@ -436,15 +450,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
           for (int j = 0; j < 4; ++j) v[j][0] = w[j * kBlkRows], v[j][1] = w[j * kBlkRows + 32];
           uint32_t x[4];  // (of a token: lane = its column)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) x[j] = lane < P.m && 4 * s + j < chunks ? tok_scales[(4 * s + j) * P.m + lane] : 0u;
-          if (it >= slots) {
-            if (!mbar_wait_warp(&sm.empty[this_e], this_epar)) {
-              if (lane == 0) flag_error(P.st, MOE_ERR_TIMEOUT, 0x514u);
-              ok = false;
-              break;
-            }
-            tc_fence_after();
-          }
+          for (int j = 0; j < 4; ++j) x[j] = lane < P.tok_rows && 4 * s + j < chunks ? tok_scales[(4 * s + j) * P.tok_rows + lane] : 0u;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             few_st4(quarter + (uint32_t)kSlotCols * this_sc + 4u * j, v[j][0], v[j][1], 0u, 0u);
@@ -470,7 +476,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
         ok = epilogue_all(ok);
         if (!ok) break;
         tc_fence_after();
-        float(*const acc)[kBlkRows] = sm.acc[buf];
+        float(*const acc)[kBlkRows] = reinterpret_cast<float(*)[kBlkRows]>(accs + buf * P.m * kBlkRows);
 #pragma unroll 1
         for (int c = 0; c < have; c += 16) {
           uint32_t v[16];
@@ -547,19 +553,24 @@ __global__ void __launch_bounds__(kFewThreads, 1)
 
 // ---------------------------------------------------------------- host
 struct FewPlan {
-  int m, stages;
+  int m, tok_rows, stages;
   size_t smem;
 };
-// Whether rows of K values fit beside a ring of four stages at least.
+// Whether rows of K values, n at most of an expert, fit beside a ring of four stages at least.  Half of an SM's shared memory where
+// that will do: the next kernel's CTAs then start beside this one's, and the down matrices are on their way while the hidden rows are
+// still being made.
 bool few_plan(const moe_ctx* ctx, int K, int n, FewPlan* plan) {
   const int chunks = (K + 127) / 128;
-  plan->m = n <= 16 ? 16 : 32;
+  plan->m = n <= 16 ? 16 : 32, plan->tok_rows = n <= 8 ? 8 : plan->m;
   // (the last stage's lower half reads up to 7 KB behind the ring)
-  const size_t toks = std::max<size_t>((size_t)((chunks + 1) / 2) * plan->m * 128 + (size_t)chunks * plan->m * 4, 8192);
-  const size_t room = (size_t)ctx->max_smem_optin - sizeof(FewSmem) - 2048;
-  if (toks + 4 * kFewStage > room) return false;
-  plan->stages = (int)std::min<size_t>(kFewStages, (room - toks) / kFewStage);
-  plan->smem = 1024 + ((size_t)plan->stages * kFewStage + 1023) / 1024 * 1024 + toks;
+  const size_t toks = (size_t)((chunks + 1) / 2) * plan->tok_rows * 128 + (size_t)chunks * plan->tok_rows * 4;
+  const size_t rest = std::max<size_t>(toks + (size_t)2 * plan->m * kBlkRows * 4, 8192) + 2048;
+  const size_t all = (size_t)ctx->max_smem_optin - sizeof(FewSmem);
+  const size_t half = (size_t)(ctx->max_smem_optin + 1024) / 2 - 1024 - sizeof(FewSmem);  // (1 KB of each CTA is the system's)
+  const size_t room = rest + 4 * kFewStage <= half ? half : all;
+  if (rest + 4 * kFewStage > room) return false;
+  plan->stages = (int)std::min<size_t>(kFewStages, (room - rest) / kFewStage);
+  plan->smem = plan->stages * (size_t)kFewStage + rest;
   return true;
 }
 
@@ -590,7 +601,7 @@ int few_launch(moe_ctx* ctx, const moe_fp4* w, FewParams& P, const FewPlan& plan
   P.K = w->n, P.w = fp4_shape(w->rows, w->n), P.N = (int)(w->rows / P.E);
   const int all = (P.K + kStageK - 1) / kStageK;
   P.part_stages = (all + P.splits - 1) / P.splits, P.splits = (all + P.part_stages - 1) / P.part_stages;
-  P.units = (P.N + kBlkRows - 1) / kBlkRows, P.stages = plan.stages, P.m = plan.m, P.st = ctx->d_state;
+  P.units = (P.N + kBlkRows - 1) / kBlkRows, P.stages = plan.stages, P.m = plan.m, P.tok_rows = plan.tok_rows, P.st = ctx->d_state;
   MOE_TRY((allow_full_smem<fp4_few_kernel<MODE>>(ctx)));
   const int most = std::min(P.E, P.n);  // experts with rows
   const long long items = (long long)P.units * P.splits * most;

@@ -40,6 +40,8 @@ constexpr uint32_t kStageBytes4 = (kSWOff4 + 2 * kMaxBn * 4 + 1023) / 1024 * 102
 constexpr int kScaleCol = 2 * kMaxBn;   // first column of the scales; a stage: A 4 + 4, W 8 + 8 columns
 constexpr int kScaleCols = 24;
 constexpr int kScaleSlots = 5;
+// (a set of scale warps meets every stage of its ring places: it must not skip a phase of their barriers)
+static_assert(kStages4 % kScaleSets == 0, "stages");
 static_assert(kScaleCol + kScaleSlots * kScaleCols <= kTmemCols && kScaleSlots < kStages4, "tensor memory");
 constexpr int kEpiBuf4 = 4096;
 
