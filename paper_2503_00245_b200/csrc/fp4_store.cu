@@ -26,29 +26,16 @@ __device__ __forceinline__ long long source_row(const int32_t* row_of, int row_d
   return r >= 0 && r < src_rows && (!row_of || row_of[i] >= 0) ? r : -1;  // (-1: a row of zeros)
 }
 
-// Rows whose values lie side by side, n a multiple of 8, 16-byte aligned: a warp takes 256 values of a row, eight to a lane.
+// Rows whose values lie side by side, n a multiple of 8, 16-byte aligned: a warp goes along a row, 256 values (eight to a lane) at a
+// time with four such steps' loads on their way; gridDim.y warps share a row where there are few.  (A warp per 256 values, its row
+// by a 64-bit division: 46080 x 2048 bf16 and back 152 us.)
+constexpr int kFly = 4;
 template <typename T>
-__global__ void __launch_bounds__(kQWarps * 32)
-    fp4_quantize_kernel(const T* __restrict__ src, long long row_stride, long long src_rows, const int32_t* __restrict__ row_of, int row_div,
-                        long long rows, int n, int units, unsigned char* __restrict__ codes, uint32_t* __restrict__ scales, Fp4Shape sh) {
-  const int lane = threadIdx.x & 31;
-  pdl_launch_dependents();
-  pdl_wait();
-  const long long id = (long long)blockIdx.x * kQWarps + (threadIdx.x >> 5);
-  const long long i = id / units;
-  const int u = (int)(id - i * units);
-  if (i >= rows) return;
-  const long long r = source_row(row_of, row_div, src_rows, i);
-  const int c = u * 256 + lane * 8;  // first of the lane's values
-  float f[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) f[j] = 0.f;
-  if (r >= 0 && c < n) load8(src + r * row_stride + c, f);
-  float m = 0.f;
+__device__ __forceinline__ void quantize_step(const float (&f)[8], int c, long long i, int n, int lane, unsigned char* codes, uint32_t* scales,
+                                              const Fp4Shape& sh) {
   uint32_t top = 0u;  // (as bits: a NaN is larger than everything)
 #pragma unroll
   for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(f[j]) & 0x7fffffffu);
-  (void)m;
   top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
   top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
   const uint32_t s = fp4_scale_byte(top);
@@ -58,6 +45,31 @@ __global__ void __launch_bounds__(kQWarps * 32)
   w |= __shfl_xor_sync(0xffffffffu, w, 4);
   w |= __shfl_xor_sync(0xffffffffu, w, 8);
   if ((lane & 15) == 0 && c < n) scales[(long long)(c >> 7) * sh.rp + i] = w;
+}
+template <typename T>
+__global__ void __launch_bounds__(kQWarps * 32)
+    fp4_quantize_kernel(const T* __restrict__ src, long long row_stride, long long src_rows, const int32_t* __restrict__ row_of, int row_div,
+                        long long rows, int n, unsigned char* __restrict__ codes, uint32_t* __restrict__ scales, Fp4Shape sh) {
+  const int lane = threadIdx.x & 31;
+  pdl_launch_dependents();
+  pdl_wait();
+  for (long long i = (long long)blockIdx.x * kQWarps + (threadIdx.x >> 5); i < rows; i += (long long)gridDim.x * kQWarps) {
+    const long long r = source_row(row_of, row_div, src_rows, i);
+    const T* const row = src + (r < 0 ? 0 : r) * row_stride;
+#pragma unroll 1
+    for (int c0 = blockIdx.y * (256 * kFly) + lane * 8; c0 - lane * 8 < n; c0 += gridDim.y * (256 * kFly)) {
+      float f[kFly][8];
+#pragma unroll
+      for (int u = 0; u < kFly; ++u) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[u][j] = 0.f;
+        if (r >= 0 && c0 + 256 * u < n) load8(row + c0 + 256 * u, f[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < kFly; ++u)
+        if (c0 - lane * 8 + 256 * u < n) quantize_step<T>(f[u], c0 + 256 * u, i, n, lane, codes, scales, sh);
+    }
+  }
 }
 
 // Any strides: a thread takes a block of 32 values of a row, neighbouring threads neighbouring rows (matrices stored with their
@@ -105,22 +117,39 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, const float* f) {
 }
 template <typename T>
 __global__ void __launch_bounds__(kQWarps * 32)
-    fp4_dequantize_kernel(const unsigned char* __restrict__ codes, const uint32_t* __restrict__ scales, long long rows, int n, int units,
+    fp4_dequantize_kernel(const unsigned char* __restrict__ codes, const uint32_t* __restrict__ scales, long long rows, int n,
                           T* __restrict__ dst, long long row_stride, Fp4Shape sh) {
   const int lane = threadIdx.x & 31;
   pdl_launch_dependents();
   pdl_wait();
-  const long long id = (long long)blockIdx.x * kQWarps + (threadIdx.x >> 5);
-  const long long i = id / units;
-  const int c = (int)(id - i * units) * 256 + lane * 8;
-  if (i >= rows || c >= n) return;
-  const uint32_t w = __ldcg(reinterpret_cast<const uint32_t*>(codes + i * sh.pitch + c / 2));
-  const uint32_t sw = __ldcg(scales + (long long)(c >> 7) * sh.rp + i);
-  const float s = fp4_scales2((sw >> (8 * ((c >> 5) & 3))) & 0xffu).x;
-  float f[8];
+  for (long long i = (long long)blockIdx.x * kQWarps + (threadIdx.x >> 5); i < rows; i += (long long)gridDim.x * kQWarps) {
+#pragma unroll 1
+    for (int c0 = blockIdx.y * (256 * kFly) + lane * 8; c0 < n; c0 += gridDim.y * (256 * kFly)) {
+      uint32_t w[kFly], sw[kFly];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) f[j] = fp4_value((w >> (4 * j)) & 15u) * s;  // (a value and a power of two: exact in either type)
-  store8(dst + i * row_stride + c, f);
+      for (int u = 0; u < kFly; ++u) {
+        const int c = min(c0 + 256 * u, n - 8);
+        w[u] = __ldcg(reinterpret_cast<const uint32_t*>(codes + i * sh.pitch + c / 2));
+        sw[u] = __ldcg(scales + (long long)(c >> 7) * sh.rp + i);
+      }
+#pragma unroll
+      for (int u = 0; u < kFly; ++u) {
+        const int c = c0 + 256 * u;
+        if (c >= n) break;
+        const float s = fp4_scales2((sw[u] >> (8 * ((c >> 5) & 3))) & 0xffu).x;
+        float f[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = fp4_value((w[u] >> (4 * j)) & 15u) * s;  // (a value and a power of two: exact in either type)
+        store8(dst + i * row_stride + c, f);
+      }
+    }
+  }
+}
+// Blocks along the rows, and warps to share a row.
+dim3 row_grid(long long rows, int n) {
+  const long long x = std::min<long long>((rows + kQWarps - 1) / kQWarps, 148 * 8);
+  const int most = (n + 256 * kFly - 1) / (256 * kFly);
+  return dim3((unsigned)x, (unsigned)std::max(1, (int)std::min<long long>(most, 148 * 4 / x)));
 }
 
 template <typename T>
@@ -130,11 +159,8 @@ int quantize_t(const Fp4Source& q, long long rows, int n, void* codes, void* sca
   const T* base = (const T*)q.base;
   const bool wide = split < 0 && q.col_stride == 1 && n % 8 == 0 && (q.row_stride * (long long)sizeof(T)) % 16 == 0 && ((uintptr_t)base & 15u) == 0;
   if (wide) {
-    const int units = (sh.nb * 32 + 255) / 256;
-    const long long blocks = (rows * units + kQWarps - 1) / kQWarps;
-    if (blocks > 0x7fffffffll) return MOE_ERR_UNSUPPORTED;
-    MOE_CUDA_TRY(launch_pdl(fp4_quantize_kernel<T>, dim3((unsigned)blocks), dim3(kQWarps * 32), 0, s, base, q.row_stride, q.rows, q.row_of,
-                            q.row_div, rows, n, units, (unsigned char*)codes, (uint32_t*)scales, sh));
+    MOE_CUDA_TRY(launch_pdl(fp4_quantize_kernel<T>, row_grid(rows, n), dim3(kQWarps * 32), 0, s, base, q.row_stride, q.rows, q.row_of,
+                            q.row_div, rows, n, (unsigned char*)codes, (uint32_t*)scales, sh));
     return MOE_OK;
   }
   const long long blocks = (rows + 255) / 256;
@@ -192,18 +218,15 @@ int moe_fp4_dequantize_rows(const moe_fp4* m, void* dst, int32_t dtype, int64_t 
       (row_stride * size) % 16)
     return MOE_ERR_INVALID_ARG;
   const Fp4Shape sh = fp4_shape(m->rows, m->n);
-  const int units = (m->n + 255) / 256;
-  const long long blocks = (m->rows * units + kQWarps - 1) / kQWarps;
-  if (blocks > 0x7fffffffll) return MOE_ERR_UNSUPPORTED;
-  const dim3 grid((unsigned)blocks), block(kQWarps * 32);
+  const dim3 grid = row_grid(m->rows, m->n), block(kQWarps * 32);
   const auto* c = (const unsigned char*)m->codes;
   const auto* sc = (const uint32_t*)m->scales;
   if (dtype == MOE_F32)
-    MOE_CUDA_TRY(launch_pdl(fp4_dequantize_kernel<float>, grid, block, 0, (cudaStream_t)stream, c, sc, (long long)m->rows, m->n, units,
+    MOE_CUDA_TRY(launch_pdl(fp4_dequantize_kernel<float>, grid, block, 0, (cudaStream_t)stream, c, sc, (long long)m->rows, m->n,
                             (float*)dst, (long long)row_stride, sh));
   else
     MOE_CUDA_TRY(launch_pdl(fp4_dequantize_kernel<__nv_bfloat16>, grid, block, 0, (cudaStream_t)stream, c, sc, (long long)m->rows, m->n,
-                            units, (__nv_bfloat16*)dst, (long long)row_stride, sh));
+                            (__nv_bfloat16*)dst, (long long)row_stride, sh));
   return MOE_OK;
 }
 
