@@ -77,6 +77,9 @@ struct Fp4Source {
 };
 // Destination rows: i, or, with `split` 0 or 1, row i of a matrix whose blocks of 32 rows alternate with another's.
 int launch_fp4_quantize(const Fp4Source& src, long long rows, int n, void* codes, void* scales, long long rp, int split, cudaStream_t s);
+// Rows of x quantised and placed by expert (offsets, and each pair's slot in inv).
+int launch_fp4_place(moe_ctx* ctx, const void* x, const int32_t* idx, int T, int32_t* offsets, int32_t* inv, void* codes, void* scales,
+                     cudaStream_t s);
 
 // csrc/fp4_few.cu: few rows (decode)
 constexpr int kFewSplits = 4;  // parts of the down product's contraction, at most

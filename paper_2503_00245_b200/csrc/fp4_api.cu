@@ -17,7 +17,7 @@ int check_matrix(const moe_fp4* m) {
 
 // Scratch of moe_fp4_experts.
 struct Fp4Ws {
-  size_t offsets, perm, inv;
+  size_t offsets, inv;
   size_t x_codes, x_scales, h_codes, h_scales, out_slots, arrived, total;
 };
 Fp4Ws fp4_ws(const moe_config& c, int T) {
@@ -31,7 +31,7 @@ Fp4Ws fp4_ws(const moe_config& c, int T) {
   const long long n = (long long)T * c.top_k;
   const Fp4Shape x = fp4_shape(n, c.d_model), h = fp4_shape(n, c.d_ff);
   L.offsets = take((size_t)(c.n_experts + 1) * 4);
-  L.perm = take((size_t)n * 4), L.inv = take((size_t)n * 4);
+  L.inv = take((size_t)n * 4);
   L.x_codes = take((size_t)n * x.pitch), L.x_scales = take((size_t)x.chunks * x.rp * 4);
   L.h_codes = take((size_t)n * h.pitch), L.h_scales = take((size_t)h.chunks * h.rp * 4);
   // (few tokens: planes of the down product's parts)
@@ -102,13 +102,9 @@ int moe_fp4_experts(moe_ctx* ctx, const void* x, int32_t T, const moe_fp4* gu, c
   float* const o = (float*)(b + L.out_slots);
   if (T <= MOE_STREAM_MAX_TOKENS && fp4_few_applies(ctx, c.d_model, T) && fp4_few_applies(ctx, c.d_ff, T))
     return launch_fp4_few_experts(ctx, x, T, gu, down, topk_idx, topk_w, y, &h, o, (unsigned*)(b + L.arrived), s);
-  int32_t *offsets = (int32_t*)(b + L.offsets), *perm = (int32_t*)(b + L.perm), *inv = (int32_t*)(b + L.inv);
-  rc = launch_permute(ctx, topk_idx, T, offsets, perm, inv, s);
+  int32_t *offsets = (int32_t*)(b + L.offsets), *inv = (int32_t*)(b + L.inv);
+  rc = launch_fp4_place(ctx, x, topk_idx, T, offsets, inv, b + L.x_codes, b + L.x_scales, s);
   if (rc != MOE_OK) return rc;
-  rc = launch_fp4_quantize(Fp4Source{x, c.x_dtype, c.d_model, 1, T, perm, c.top_k}, n, c.d_model, b + L.x_codes, b + L.x_scales,
-                           fp4_shape(n, c.d_model).rp, -1, s);
-  if (rc != MOE_OK) return rc;
-  ctx->launches++;
   rc = launch_fp4_tensor(ctx, &xq, gu, offsets, c.n_experts, nullptr, 0, 0, &h, s);
   if (rc != MOE_OK) return rc;
   rc = launch_fp4_tensor(ctx, &h, down, offsets, c.n_experts, o, 1, c.d_model, nullptr, s);

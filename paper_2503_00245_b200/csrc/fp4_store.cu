@@ -30,21 +30,23 @@ __device__ __forceinline__ long long source_row(const int32_t* row_of, int row_d
 // time with four such steps' loads on their way; gridDim.y warps share a row where there are few.  (A warp per 256 values, its row
 // by a 64-bit division: 46080 x 2048 bf16 and back 152 us.)
 constexpr int kFly = 4;
-template <typename T>
-__device__ __forceinline__ void quantize_step(const float (&f)[8], int c, long long i, int n, int lane, unsigned char* codes, uint32_t* scales,
-                                              const Fp4Shape& sh) {
+__device__ __forceinline__ void quantize_step(const float (&f)[8], int c, int lane, const Fp4Shape& sh, uint32_t& word, uint32_t& scale) {
   uint32_t top = 0u;  // (as bits: a NaN is larger than everything)
 #pragma unroll
   for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(f[j]) & 0x7fffffffu);
   top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
   top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
   const uint32_t s = fp4_scale_byte(top);
-  if (c < 32 * sh.nb) *reinterpret_cast<uint32_t*>(codes + i * sh.pitch + c / 2) = fp4_pack8(f, fp4_up(s));
+  word = fp4_pack8(f, fp4_up(s));
   // a word of scales: four blocks, sixteen lanes
-  uint32_t w = c < 32 * sh.nb ? s << (8 * ((lane >> 2) & 3)) : 0u;
-  w |= __shfl_xor_sync(0xffffffffu, w, 4);
-  w |= __shfl_xor_sync(0xffffffffu, w, 8);
-  if ((lane & 15) == 0 && c < n) scales[(long long)(c >> 7) * sh.rp + i] = w;
+  scale = c < 32 * sh.nb ? s << (8 * ((lane >> 2) & 3)) : 0u;
+  scale |= __shfl_xor_sync(0xffffffffu, scale, 4);
+  scale |= __shfl_xor_sync(0xffffffffu, scale, 8);
+}
+__device__ __forceinline__ void store_step(uint32_t word, uint32_t scale, int c, long long i, int n, int lane, unsigned char* codes,
+                                           uint32_t* scales, const Fp4Shape& sh) {
+  if (c < 32 * sh.nb) *reinterpret_cast<uint32_t*>(codes + i * sh.pitch + c / 2) = word;
+  if ((lane & 15) == 0 && c < n) scales[(long long)(c >> 7) * sh.rp + i] = scale;
 }
 template <typename T>
 __global__ void __launch_bounds__(kQWarps * 32)
@@ -67,7 +69,11 @@ __global__ void __launch_bounds__(kQWarps * 32)
       }
 #pragma unroll
       for (int u = 0; u < kFly; ++u)
-        if (c0 - lane * 8 + 256 * u < n) quantize_step<T>(f[u], c0 + 256 * u, i, n, lane, codes, scales, sh);
+        if (c0 - lane * 8 + 256 * u < n) {
+          uint32_t word, scale;
+          quantize_step(f[u], c0 + 256 * u, lane, sh, word, scale);
+          store_step(word, scale, c0 + 256 * u, i, n, lane, codes, scales, sh);
+        }
     }
   }
 }
@@ -171,6 +177,116 @@ int quantize_t(const Fp4Source& q, long long rows, int n, void* codes, void* sca
   return MOE_OK;
 }
 
+// ---- rows of many tokens on their way to their experts: grouping and quantisation in one launch
+// Pairs (token, choice) are numbered in order; a pair's slot is its expert's first slot plus the number of earlier pairs of that expert.
+// Every CTA counts the pairs of all tokens by expert, those in front of its own tokens apart (n words from L2), ranks its own, and writes each of its tokens' rows, quantised once, to the token's k slots.  So no CTA waits
+// for another and nothing is left to clear.  (A grouping launch of one CTA and a gathering one: 18 us for 2048 tokens, two experts each.)
+constexpr int kPlaceWarps = 8;
+struct PlaceParams {
+  const void* x;
+  const int32_t* idx;
+  int T, k, E, d, tokens;  // tokens of a CTA
+  int32_t *offsets, *inv;
+  unsigned char* codes;
+  uint32_t* scales;
+  Fp4Shape sh;
+  DeviceState* st;
+};
+template <typename T>
+__global__ void __launch_bounds__(kPlaceWarps * 32) fp4_place_kernel(const PlaceParams P) {
+  extern __shared__ int s_slot[];  // [tokens][k]
+  __shared__ int s_all[kPlaceWarps][MOE_MAX_EXPERTS], s_before[kPlaceWarps][MOE_MAX_EXPERTS], s_next[MOE_MAX_EXPERTS];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  pdl_launch_dependents();
+  for (int i = tid; i < kPlaceWarps * MOE_MAX_EXPERTS; i += kPlaceWarps * 32) (&s_all[0][0])[i] = 0, (&s_before[0][0])[i] = 0;
+  __syncthreads();
+  pdl_wait();
+  const int t0 = blockIdx.x * P.tokens, t1 = min(t0 + P.tokens, P.T), n = P.T * P.k, own = t0 * P.k;
+  auto expert = [&](int p) {  // -1: none
+    const int e = p < n ? __ldcg(P.idx + p) : -1;
+    return e >= 0 && e < P.E ? e : -1;
+  };
+  // ---- the warp's first row is on its way while the pairs are counted
+  const int parts = (P.d + 256 * kFly - 1) / (256 * kFly), tasks = (t1 - t0) * parts;
+  float f[kFly][8];
+  auto fetch = [&](int i) {
+    const int t = i / parts, c0 = (i - t * parts) * 256 * kFly + lane * 8;
+    const T* row = (const T*)P.x + (long long)(t0 + t) * P.d;
+#pragma unroll
+    for (int u = 0; u < kFly; ++u) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[u][j] = 0.f;
+      if (c0 + 256 * u < P.d) load8(row + c0 + 256 * u, f[u]);
+    }
+  };
+  if (warp < tasks) fetch(warp);
+  // ---- counts, by the warps' own counters; eight loads on their way
+  const unsigned below = (1u << lane) - 1u;
+  constexpr int kPairs = 8;
+  for (int p0 = tid; p0 < n; p0 += kPairs * kPlaceWarps * 32) {
+    int e[kPairs];
+#pragma unroll
+    for (int u = 0; u < kPairs; ++u) e[u] = expert(p0 + u * kPlaceWarps * 32);
+#pragma unroll
+    for (int u = 0; u < kPairs; ++u)
+      if (e[u] >= 0) {
+        atomicAdd(&s_all[warp][e[u]], 1);
+        if (p0 + u * kPlaceWarps * 32 < own) atomicAdd(&s_before[warp][e[u]], 1);
+      }
+  }
+  __syncthreads();
+  if (warp == 0) {  // first slots of the experts, and of this CTA's pairs among theirs
+    int all[2] = {0, 0}, before[2] = {0, 0};
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      for (int w = 0; w < kPlaceWarps; ++w) all[h] += s_all[w][lane + 32 * h], before[h] += s_before[w][lane + 32 * h];
+    int a0 = all[0], a1 = all[1];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v0 = __shfl_up_sync(0xffffffffu, a0, o), v1 = __shfl_up_sync(0xffffffffu, a1, o);
+      if (lane >= o) a0 += v0, a1 += v1;
+    }
+    const int half = __shfl_sync(0xffffffffu, a0, 31), total = half + __shfl_sync(0xffffffffu, a1, 31);
+    a0 -= all[0], a1 += half - all[1];
+    s_next[lane] = a0 + before[0], s_next[lane + 32] = a1 + before[1];
+    if (blockIdx.x == 0) {
+      if (lane < P.E) P.offsets[lane] = a0;
+      if (lane + 32 < P.E) P.offsets[lane + 32] = a1;
+      if (lane == 0) P.offsets[P.E] = total;
+    }
+    __syncwarp();
+    // ---- slots of the CTA's own pairs, in order
+    const int mine = (t1 - t0) * P.k;
+    for (int p0 = 0; p0 < mine; p0 += 32) {
+      const int p = p0 + lane, e = p < mine ? expert(own + p) : -1;
+      if (p < mine && e < 0) flag_error(P.st, MOE_ERR_STATE, 0x530u);
+      const unsigned peers = __match_any_sync(0xffffffffu, e);
+      const int slot = e >= 0 ? s_next[e] + __popc(peers & below) : -1;
+      __syncwarp();
+      if (e >= 0 && (peers & below) == 0u) s_next[e] += __popc(peers);
+      __syncwarp();
+      if (p < mine) s_slot[p] = slot, P.inv[own + p] = max(slot, 0);  // (a pair without an expert: any slot, its token is undefined)
+    }
+  }
+  __syncthreads();
+  // ---- the rows: a warp for 1024 values of a token
+  for (int i = warp; i < tasks; i += kPlaceWarps) {
+    const int t = i / parts, c0 = (i - t * parts) * 256 * kFly + lane * 8;
+    if (i != warp) fetch(i);
+#pragma unroll
+    for (int u = 0; u < kFly; ++u) {
+      const int c = c0 + 256 * u;
+      if (c - lane * 8 >= P.d) break;
+      uint32_t word, scale;
+      quantize_step(f[u], c, lane, P.sh, word, scale);
+      for (int j = 0; j < P.k; ++j) {
+        const int slot = s_slot[t * P.k + j];
+        if (slot >= 0) store_step(word, scale, c, slot, P.d, lane, P.codes, P.scales, P.sh);
+      }
+    }
+  }
+}
+
 bool misaligned(const void* p) { return ((uintptr_t)p & 15u) != 0; }
 
 }  // namespace
@@ -179,6 +295,23 @@ int launch_fp4_quantize(const Fp4Source& src, long long rows, int n, void* codes
   if (rows <= 0) return MOE_OK;
   return src.dtype == MOE_F32 ? quantize_t<float>(src, rows, n, codes, scales, rp, split, s)
                               : quantize_t<__nv_bfloat16>(src, rows, n, codes, scales, rp, split, s);
+}
+
+int launch_fp4_place(moe_ctx* ctx, const void* x, const int32_t* idx, int T, int32_t* offsets, int32_t* inv, void* codes, void* scales,
+                     cudaStream_t s) {
+  const moe_config& c = ctx->cfg;
+  PlaceParams P{x, idx, T, c.top_k, c.n_experts, c.d_model, 0, offsets, inv, (unsigned char*)codes, (uint32_t*)scales,
+                fp4_shape((long long)T * c.top_k, c.d_model), ctx->d_state};
+  // two CTAs to an SM, or more tokens each where there are many
+  P.tokens = std::max(2, std::min((T + 2 * ctx->sm_count - 1) / (2 * ctx->sm_count), 1024));
+  const dim3 grid((unsigned)((T + P.tokens - 1) / P.tokens)), block(kPlaceWarps * 32);
+  const size_t smem = (size_t)P.tokens * c.top_k * 4;
+  if (c.x_dtype == MOE_F32)
+    MOE_CUDA_TRY(launch_pdl(fp4_place_kernel<float>, grid, block, smem, s, P));
+  else
+    MOE_CUDA_TRY(launch_pdl(fp4_place_kernel<__nv_bfloat16>, grid, block, smem, s, P));
+  ctx->launches++;
+  return MOE_OK;
 }
 
 }  // namespace cosmoe

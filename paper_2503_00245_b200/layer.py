@@ -51,13 +51,16 @@ class Fp4Rows:
     @classmethod
     def empty(cls, rows, n, device="cuda"):
         nb = -(-n // 32)
-        return cls(torch.empty((rows, 16 * nb), dtype=torch.uint8, device=device),
-                   torch.empty((-(-nb // 4), -(-rows // 4) * 4, 4), dtype=torch.uint8, device=device), n)
+        q = object.__new__(cls)  # (what it allocates itself needs no checks: they take longer than a small matrix)
+        q.codes = codes = torch.empty((rows, 16 * nb), dtype=torch.uint8, device=device)
+        q.scales = scales = torch.empty((-(-nb // 4), -(-rows // 4) * 4, 4), dtype=torch.uint8, device=device)
+        q.rows, q.n, q.c = rows, n, B.moe_fp4(codes.data_ptr(), scales.data_ptr(), rows, n)
+        return q
 
     def dequantize(self, dtype=torch.bfloat16):
         """The values, [rows, n] (n a multiple of 8)."""
         out = torch.empty((self.rows, self.n), dtype=dtype, device=self.codes.device)
-        _here(self.codes)
+        _here(out)
         B.moe_fp4_dequantize_rows(self.c, out)
         return out
 
@@ -81,7 +84,7 @@ def fp4_quantize(x, row_of=None, row_div=1):
         rows = row_of.shape[0]
     _here(x, row_of)
     q = Fp4Rows.empty(rows, x.shape[1], x.device)
-    B.moe_fp4_quantize_rows(x, row_of, row_div, rows, q.codes, q.scales)
+    B.moe_fp4_quantize_rows(x, row_of, row_div, rows, q.c.codes, q.c.scales)
     return q
 
 
@@ -136,14 +139,15 @@ class SelectRule:
 
 def select_experts(logits, rule: SelectRule, bias=None):
     """logits [T, E] float32 or bfloat16 (rows may lie apart), bias [E] float32 -> (topk_idx int32 [T, k], topk_w float32 [T, k])."""
-    if logits.dim() != 2 or logits.shape[1] != rule.E or (rule.E > 1 and logits.stride(1) != 1):
+    shape = logits.shape
+    if len(shape) != 2 or shape[1] != rule.E or (rule.E > 1 and logits.stride(1) != 1):
         raise ValueError(f"logits have to be [T, {rule.E}] with contiguous rows")
     if bias is not None and (bias.dtype != torch.float32 or bias.shape != (rule.E,)):
         raise ValueError(f"the bias has to be float32 [{rule.E}]")
     _here(logits, bias)
-    T = logits.shape[0]
-    idx = torch.empty((T, rule.k), dtype=torch.int32, device=logits.device)
-    w = torch.empty((T, rule.k), dtype=torch.float32, device=logits.device)
+    T, device = shape[0], logits.device
+    idx = torch.empty((T, rule.k), dtype=torch.int32, device=device)
+    w = torch.empty((T, rule.k), dtype=torch.float32, device=device)
     B.moe_select(rule.c, logits, T, bias, idx, w, logits.stride(0) if T > 1 else rule.E)
     return idx, w
 
