@@ -47,21 +47,33 @@ __device__ __forceinline__ uint32_t fp4_pack8(const float* v, float up) {
                    : fp4_pack2(v[0] * up, v[1] * up) | fp4_pack2(v[2] * up, v[3] * up) << 8 |
                          fp4_pack2(v[4] * up, v[5] * up) << 16 | fp4_pack2(v[6] * up, v[7] * up) << 24;
 }
-// 2^(s - 127) of the two scale bytes in the low half of a word (0: 2^-127; 255: NaN).
-__device__ __forceinline__ float2 fp4_scales2(uint32_t two) {
+// 2^(s - 127) of a scale byte, twice, in bf16 (0: 2^-127; 255: NaN).
+__device__ __forceinline__ uint32_t fp4_scale_bf16x2(uint32_t s) {
   uint32_t r;
-  asm("{\n\t.reg .b16 h;\n\tcvt.u16.u32 h, %1;\n\tcvt.rn.bf16x2.ue8m0x2 %0, h;\n\t}" : "=r"(r) : "r"(two));
-  return make_float2(__uint_as_float(r << 16), __uint_as_float(r & 0xffff0000u));
+  asm("{\n\t.reg .b16 h;\n\tcvt.u16.u32 h, %1;\n\tcvt.rn.bf16x2.ue8m0x2 %0, h;\n\t}" : "=r"(r) : "r"(s | s << 8));
+  return r;
 }
-// Eight codes as E4M3 bytes (values 0, 2, 4, 6 and 1, 3, 5, 7): the code's exponent and mantissa bits in the places of E4M3's
-// lowest exponent and highest mantissa bits, zeros and halves included, are the value times 2^-6.
-__device__ __forceinline__ uint32_t fp4_even_e4m3(uint32_t w) { return ((w << 4) & 0x80808080u) | ((w << 2) & 0x1c1c1c1cu); }
-__device__ __forceinline__ uint32_t fp4_odd_e4m3(uint32_t w) { return (w & 0x80808080u) | ((w >> 2) & 0x1c1c1c1cu); }
-// A code's value.
-__device__ __forceinline__ float fp4_value(uint32_t c) {
-  const uint32_t e = (c >> 1) & 3u, m = c & 1u;
-  const float mag = e == 0u ? 0.5f * (float)m : __uint_as_float(((e + 126u) << 23) | (m << 22));
-  return (c & 8u) ? -mag : mag;
+// Eight codes' values as bf16 pairs, in order: the bytes of a magnitude's bf16 are looked up by byte permutes (a selector takes three
+// bits of a code), its sign is the top bit of a byte of the word or of the word shifted by four.
+__device__ __forceinline__ void fp4_bf16(uint32_t w, uint32_t (&out)[4]) {
+  const uint32_t up = w << 4;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t sel = (h ? w >> 16 : w) & 0x7777u;
+    const uint32_t hi = __byte_perm(0x3f3f3f00u, 0x40404040u, sel), lo = __byte_perm(0xc0800000u, 0xc0804000u, sel);
+    const uint32_t top = hi | (__byte_perm(up, w, h ? 0xfbeau : 0xd9c8u) & 0x80808080u);
+    out[2 * h] = __byte_perm(lo, top, 0x5140), out[2 * h + 1] = __byte_perm(lo, top, 0x7362);
+  }
+}
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
 }
 
 #endif  // __CUDACC__

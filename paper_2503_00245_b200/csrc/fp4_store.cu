@@ -13,11 +13,58 @@ namespace {
 
 constexpr int kQWarps = 8;
 
-__device__ __forceinline__ void load8(const float* p, float* f) {
-  const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
-  f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+// Eight values of a row, as they come from memory.
+struct Eight32 {
+  float4 a, b;
+};
+struct Eight16 {
+  uint4 w;
+};
+template <typename T>
+struct EightOf;
+template <>
+struct EightOf<float> {
+  typedef Eight32 type;
+};
+template <>
+struct EightOf<__nv_bfloat16> {
+  typedef Eight16 type;
+};
+__device__ __forceinline__ Eight32 load8(const float* p) {
+  return Eight32{__ldg(reinterpret_cast<const float4*>(p)), __ldg(reinterpret_cast<const float4*>(p) + 1)};
 }
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, float* f) { unpack8(__ldg(reinterpret_cast<const uint4*>(p)), f); }
+__device__ __forceinline__ Eight16 load8(const __nv_bfloat16* p) { return Eight16{__ldg(reinterpret_cast<const uint4*>(p))}; }
+// The scale byte of the four lanes' block, and the lane's eight codes.
+__device__ __forceinline__ uint32_t quantize8(const Eight32& v, uint32_t& word) {
+  const float f[8] = {v.a.x, v.a.y, v.a.z, v.a.w, v.b.x, v.b.y, v.b.z, v.b.w};
+  uint32_t top = 0u;  // (as bits: a NaN is larger than everything)
+#pragma unroll
+  for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(f[j]) & 0x7fffffffu);
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+  const uint32_t s = fp4_scale_byte(top);
+  word = fp4_pack8(f, fp4_up(s));
+  return s;
+}
+// bf16 two at a time: their bits order as unsigned words do, and a product with a power of two is exact (what it may lose below
+// 2^-126 is far below the smallest code's quarter)
+__device__ __forceinline__ uint32_t quantize8(const Eight16& v, uint32_t& word) {
+  const uint32_t m = max_u16x2(max_u16x2(v.w.x & 0x7fff7fffu, v.w.y & 0x7fff7fffu), max_u16x2(v.w.z & 0x7fff7fffu, v.w.w & 0x7fff7fffu));
+  uint32_t top = max(m & 0xffffu, m >> 16);
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+  const uint32_t s = fp4_scale_byte(top << 16);
+  const uint32_t up = s == 255u ? 0u : ((254u - s) << 7) * 0x10001u;
+  const uint32_t w[4] = {v.w.x, v.w.y, v.w.z, v.w.w};
+  uint32_t q[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t p = mul_bf16x2(w[j], up);
+    q[j] = fp4_pack2(__uint_as_float(p << 16), __uint_as_float(p & 0xffff0000u));
+  }
+  word = s == 255u ? 0u : q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24;
+  return s;
+}
 __device__ __forceinline__ float one(const float* p) { return __ldg(p); }
 __device__ __forceinline__ float one(const __nv_bfloat16* p) { return bf16_to_float(__ldg(reinterpret_cast<const uint16_t*>(p))); }
 
@@ -30,14 +77,9 @@ __device__ __forceinline__ long long source_row(const int32_t* row_of, int row_d
 // time with four such steps' loads on their way; gridDim.y warps share a row where there are few.  (A warp per 256 values, its row
 // by a 64-bit division: 46080 x 2048 bf16 and back 152 us.)
 constexpr int kFly = 4;
-__device__ __forceinline__ void quantize_step(const float (&f)[8], int c, int lane, const Fp4Shape& sh, uint32_t& word, uint32_t& scale) {
-  uint32_t top = 0u;  // (as bits: a NaN is larger than everything)
-#pragma unroll
-  for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(f[j]) & 0x7fffffffu);
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-  const uint32_t s = fp4_scale_byte(top);
-  word = fp4_pack8(f, fp4_up(s));
+template <typename V>
+__device__ __forceinline__ void quantize_step(const V& v, int c, int lane, const Fp4Shape& sh, uint32_t& word, uint32_t& scale) {
+  const uint32_t s = quantize8(v, word);
   // a word of scales: four blocks, sixteen lanes
   scale = c < 32 * sh.nb ? s << (8 * ((lane >> 2) & 3)) : 0u;
   scale |= __shfl_xor_sync(0xffffffffu, scale, 4);
@@ -60,12 +102,11 @@ __global__ void __launch_bounds__(kQWarps * 32)
     const T* const row = src + (r < 0 ? 0 : r) * row_stride;
 #pragma unroll 1
     for (int c0 = blockIdx.y * (256 * kFly) + lane * 8; c0 - lane * 8 < n; c0 += gridDim.y * (256 * kFly)) {
-      float f[kFly][8];
+      typename EightOf<T>::type f[kFly];
 #pragma unroll
       for (int u = 0; u < kFly; ++u) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) f[u][j] = 0.f;
-        if (r >= 0 && c0 + 256 * u < n) load8(row + c0 + 256 * u, f[u]);
+        f[u] = {};
+        if (r >= 0 && c0 + 256 * u < n) f[u] = load8(row + c0 + 256 * u);
       }
 #pragma unroll
       for (int u = 0; u < kFly; ++u)
@@ -113,13 +154,22 @@ __global__ void __launch_bounds__(256)
   }
 }
 
-__device__ __forceinline__ void store8(float* p, const float* f) {
-  reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
-  reinterpret_cast<float4*>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+// Eight codes times their scale: a value and a power of two, exact in either type unless it overflows.
+__device__ __forceinline__ void store8(__nv_bfloat16* p, uint32_t w, uint32_t s) {
+  const uint32_t scale = fp4_scale_bf16x2(s);
+  uint32_t v[4];
+  fp4_bf16(w, v);
+  *reinterpret_cast<uint4*>(p) = make_uint4(mul_bf16x2(v[0], scale), mul_bf16x2(v[1], scale), mul_bf16x2(v[2], scale), mul_bf16x2(v[3], scale));
 }
-__device__ __forceinline__ void store8(__nv_bfloat16* p, const float* f) {
-  *reinterpret_cast<uint4*>(p) =
-      make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+__device__ __forceinline__ void store8(float* p, uint32_t w, uint32_t s) {
+  const float scale = __uint_as_float(fp4_scale_bf16x2(s) << 16);
+  uint32_t v[4];
+  fp4_bf16(w, v);
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    reinterpret_cast<float4*>(p)[h] =
+        make_float4(__uint_as_float(v[2 * h] << 16) * scale, __uint_as_float(v[2 * h] & 0xffff0000u) * scale,
+                    __uint_as_float(v[2 * h + 1] << 16) * scale, __uint_as_float(v[2 * h + 1] & 0xffff0000u) * scale);
 }
 template <typename T>
 __global__ void __launch_bounds__(kQWarps * 32)
@@ -142,11 +192,7 @@ __global__ void __launch_bounds__(kQWarps * 32)
       for (int u = 0; u < kFly; ++u) {
         const int c = c0 + 256 * u;
         if (c >= n) break;
-        const float s = fp4_scales2((sw[u] >> (8 * ((c >> 5) & 3))) & 0xffu).x;
-        float f[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = fp4_value((w[u] >> (4 * j)) & 15u) * s;  // (a value and a power of two: exact in either type)
-        store8(dst + i * row_stride + c, f);
+        store8(dst + i * row_stride + c, w[u], (sw[u] >> (8 * ((c >> 5) & 3))) & 0xffu);
       }
     }
   }
@@ -155,7 +201,7 @@ __global__ void __launch_bounds__(kQWarps * 32)
 dim3 row_grid(long long rows, int n) {
   const long long x = std::min<long long>((rows + kQWarps - 1) / kQWarps, 148 * 8);
   const int most = (n + 256 * kFly - 1) / (256 * kFly);
-  return dim3((unsigned)x, (unsigned)std::max(1, (int)std::min<long long>(most, 148 * 4 / x)));
+  return dim3((unsigned)x, (unsigned)std::max(1, (int)std::min<long long>(most, 148 * 8 / x)));
 }
 
 template <typename T>
@@ -208,15 +254,14 @@ __global__ void __launch_bounds__(kPlaceWarps * 32) fp4_place_kernel(const Place
   };
   // ---- the warp's first row is on its way while the pairs are counted
   const int parts = (P.d + 256 * kFly - 1) / (256 * kFly), tasks = (t1 - t0) * parts;
-  float f[kFly][8];
+  typename EightOf<T>::type f[kFly];
   auto fetch = [&](int i) {
     const int t = i / parts, c0 = (i - t * parts) * 256 * kFly + lane * 8;
     const T* row = (const T*)P.x + (long long)(t0 + t) * P.d;
 #pragma unroll
     for (int u = 0; u < kFly; ++u) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) f[u][j] = 0.f;
-      if (c0 + 256 * u < P.d) load8(row + c0 + 256 * u, f[u]);
+      f[u] = {};
+      if (c0 + 256 * u < P.d) f[u] = load8(row + c0 + 256 * u);
     }
   };
   if (warp < tasks) fetch(warp);
