@@ -27,7 +27,8 @@
  *    finds.  A decode call of dense experts, or of one token with decomposed experts, is a CTA per SM that wait for one another:
  *    it may run beside anything that ends by itself, prefill calls and cooperative launches included, but two such decode calls
  *    (or one and another kernel of that kind) must not overlap: each could hold SMs that the other one's missing CTAs
- *    need until both give up with MOE_ERR_TIMEOUT.  Put them on one stream, or order them with events.
+ *    need until both give up with MOE_ERR_TIMEOUT.  Put them on one stream, or order them with events.  (Calls with 4-bit experts
+ *    do not wait in that way.)
  *  - Kernels that use programmatic dependent launch overlap the end of the kernel in front of them in the stream.  What
  *    that one writes is read after it has completed, with one exception: decode calls of dense experts, and of one token,
  *    read w_router earlier.  If the kernel in front lets its successors start early (griddepcontrol.launch_dependents; this
@@ -203,8 +204,9 @@ int moe_fp4_pack_dense(int32_t d_model, int32_t d_ff, int32_t n_experts, const v
  * with the values that the codes stand for, fp32 sums, one rounding to out_dtype.  expert_offsets dev [E + 1] int32, ascending, as
  * moe_permute leaves them; with one expert, the plain product.  Rows of a before the first offset or behind the last are not read
  * and their rows of out are left as they were.  a->n == w->n, N a multiple of 8, out_stride >= N and a multiple of 8, out 16-byte
- * aligned, E <= MOE_MAX_EXPERTS.  Above MOE_FP4_FEW_ROWS rows of a on the tensor cores' 4-bit instructions, whose sums of 64
- * products are cut, not rounded; ctx holds the status word.                                                             */
+ * aligned, E <= MOE_MAX_EXPERTS.  On the tensor cores' 4-bit instructions, whose sums of 64 products are cut, not rounded; up to
+ * MOE_FP4_FEW_ROWS rows of a (and rows that are not too long) by kernels that read w once.  ctx holds the status word; calls on one ctx
+ * may overlap.                                                                                                         */
 #define MOE_FP4_FEW_ROWS 32
 int moe_fp4_product(moe_ctx* ctx, const moe_fp4* a, const moe_fp4* w, const int32_t* expert_offsets, int32_t n_experts, void* out,
                     int32_t out_dtype, int64_t out_stride, void* stream);

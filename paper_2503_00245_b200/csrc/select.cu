@@ -9,8 +9,9 @@
 //
 // One warp per token, eight experts to a lane at most.  Most tokens are decided in 32 bits: keys with a known bound on their error,
 // and only where two neighbours among the chosen (or the next one), or the last group kept and the first one left, are nearer
-// than the bound the token is decided again in 64 bits.  256 exponentials and the selection in 64 bits for every token: 68 us for
-// 16384 tokens of 256 experts in 8 groups.
+// than the bound the token is decided again in 64 bits.  What bounds it is the instructions of a token, about a thousand with 256
+// experts in groups: 16384 such tokens (8.4 MB of bf16 logits, 1.4 us of HBM) take 30 us; with all exponentials and the selection in
+// 64 bits 68, in 32 bits with a search of a lane's keys for every choice 48.
 #include <math_constants.h>
 
 #include <algorithm>
@@ -234,7 +235,7 @@ __global__ void __launch_bounds__(kSelWarps * 32) select_kernel(const SelectPara
   const float margin = by_logits ? -1.f : (1.f + most) * (256.f / 16777216.f);
 
 #pragma unroll 1
-  for (int t = blockIdx.x * kSelWarps + warp; t < P.T; t += gridDim.x * kSelWarps) {
+  for (long long t = blockIdx.x * kSelWarps + warp; t < P.T; t += gridDim.x * kSelWarps) {
     const T* row = (const T*)P.logits + t * P.stride;
     // ---- logits (NaN counts as -inf), the largest
     float l[N];
@@ -358,8 +359,8 @@ __global__ void __launch_bounds__(kSelWarps * 32) select_kernel(const SelectPara
       w = (float)(my_s * (double)c.scale);
     }
     if (lane < k) {
-      P.idx[(long long)t * k + lane] = my_e;
-      P.w[(long long)t * k + lane] = w;
+      P.idx[t * k + lane] = my_e;
+      P.w[t * k + lane] = w;
     }
   }
 }

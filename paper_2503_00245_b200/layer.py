@@ -110,7 +110,8 @@ def _shared_ctx():
 def fp4_product(a: Fp4Rows, w: Fp4Rows, expert_offsets, out=None, out_dtype=torch.bfloat16, ctx=None):
     """out[s] = a[s] times the matrix of the expert e with expert_offsets[e] <= s < expert_offsets[e + 1]; w holds the experts'
     matrices, w.rows / E rows each.  Rows outside the offsets are left as they are.  out: rows may lie apart.  Without a ctx (its
-    status word is what moe_check reads) the library's own for this device is used, made by the first call on it."""
+    status word is what moe_check reads) the library's own for this device is used, made by the first call on it: let that one come
+    before a stream is captured."""
     E = expert_offsets.shape[0] - 1
     if expert_offsets.dtype != torch.int32 or E < 1:
         raise TypeError("expert_offsets is a vector of E + 1 int32")

@@ -2,12 +2,9 @@
 
 Quantisation and reading back are exact and compared bit by bit.
 
-A product's sums: with `n` values of a row, S = sum |a w|.
-  few rows   sums of 32 products are exact, scaled by powers of two exactly, and added in fp32: at most n / 32 + 16 roundings of at
-             most 2^-24 of a partial sum each: (n / 32 + 16) 2^-24 S.
-  many rows  an instruction adds 64 products to the accumulator and cuts what does not fit: at most one unit in the last place, 2^-23
-             of the largest partial sum, for each of its 65 addends in the worst case a sum of whose cuts is 2^-22 of S per step of
-             the adder tree; n / 64 instructions: (n / 64 + 4) 2^-21 S.
+A product's sums: with `n` values of a row, S = sum |a w|.  An instruction adds 64 products to the accumulator and cuts what does
+not fit: at most one unit in the last place, 2^-23 of the largest partial sum, for each of its 65 addends in the worst case a sum of
+whose cuts is 2^-22 of S per step of the adder tree; n / 64 instructions: (n / 64 + 4) 2^-21 S.
 A rounding to bf16 adds 2^-8 of the value (half a step, torch.finfo(bfloat16).eps / 2).
 
 The experts' FFN rounds its hidden values to 4 bits.  With d_h the error a hidden value may have before that (from the bounds above,
@@ -163,11 +160,11 @@ def values(q):
     return Q.load(*parts(q), q.n)
 
 
-def check_product(a, w, offsets, E, out, few):
+def check_product(a, w, offsets, E, out):
     av, wv = values(a), values(w)
     want, most = Q.product(av, wv, offsets, E), Q.product(np.abs(av), np.abs(wv), offsets, E)
     got = host(out)
-    tol = ((a.n / 32 + 16) * 2.0 ** -24 if few else (a.n / 64 + 4) * 2.0 ** -21) * most
+    tol = (a.n / 64 + 4) * 2.0 ** -21 * most
     if out.dtype == torch.bfloat16:
         tol = tol + 2.0 ** -8 * (np.abs(want) + tol)
     inside = ~np.isnan(want)
@@ -191,7 +188,7 @@ def test_product(name, n, N, out_dtype):
     E, rows = len(offsets) - 1, offsets[-1]
     a, w = random_rows(rows, n, 1), random_rows(E * N, n, 2, n ** -0.5)
     out = P().fp4_product(a, w, torch.tensor(offsets, dtype=torch.int32).cuda(), out_dtype=out_dtype)
-    check_product(a, w, offsets, E, out, rows <= 32)
+    check_product(a, w, offsets, E, out)
     from paper_2503_00245_b200 import layer as L
     assert P().binding.moe_check(L._shared_ctx()) == 0
 
@@ -217,11 +214,11 @@ def test_rows_of_no_expert_are_left_alone(rows):
     out = torch.full((rows, 64), 7.0).cuda()
     P().fp4_product(a, w, torch.tensor(offsets, dtype=torch.int32).cuda(), out=out[:, :N])
     assert (out[:3] == 7).all() and (out[rows - 5:] == 7).all() and (out[:, N:] == 7).all()
-    check_product(a, w, offsets, E, out[:, :N], rows <= 32)
+    check_product(a, w, offsets, E, out[:, :N])
     # offsets that claim more rows than there are
     out.fill_(7.0)
     P().fp4_product(a, w, torch.tensor([-4, 10, rows + 900], dtype=torch.int32).cuda(), out=out[:, :N])
-    check_product(a, w, [0, 10, rows], E, out[:, :N], rows <= 32)
+    check_product(a, w, [0, 10, rows], E, out[:, :N])
 
 
 @pytest.mark.parametrize("rows", [6, 200])
@@ -246,7 +243,7 @@ def test_scales_at_the_ends_of_the_range(rows):
         a.scales.fill_(sa), w.scales.fill_(sw)
         a.scales[:, :, 3], w.scales[:, :, 3] = 0, 0
         out = P().fp4_product(a, w, at, out_dtype=torch.float32)
-        check_product(a, w, [0, rows], 1, out, rows <= 32)
+        check_product(a, w, [0, rows], 1, out)
 
 
 def test_products_are_the_same_again_and_wherever_a_row_stands():
@@ -281,7 +278,7 @@ def test_product_captured_and_on_two_streams():
     a.codes.copy_(random_rows(200, 256, 14).codes)
     g.replay()
     torch.cuda.synchronize()
-    check_product(a, w, [0, 50, 120, 200], 3, x, False)
+    check_product(a, w, [0, 50, 120, 200], 3, x)
     want = P().fp4_product(a, w, at)
     torch.cuda.synchronize()
     outs = []
@@ -315,13 +312,13 @@ def round4(h, s):
     return (np.sign(v) * Q.VALUES[Q.nearest_code(np.abs(v) / step)] * step).reshape(h.shape[0], -1)[:, :f]
 
 
-def expected(x, gate, up, down, idx, wt, few):
+def expected(x, gate, up, down, idx, wt):
     """(y, bound of its error before the last rounding); see the head of this file."""
     T, d = x.shape
     f = gate.shape[1]
     xq = Q.values(*Q.quantize(x), d)
     y, tol = np.zeros_like(x), np.zeros_like(x)
-    c_in, c_out = ((n / 32 + 16) * 2.0 ** -24 if few else (n / 64 + 4) * 2.0 ** -21 for n in (d, f))
+    c_in, c_out = ((n / 64 + 4) * 2.0 ** -21 for n in (d, f))
     for e in range(gate.shape[0]):
         t, j = np.nonzero(idx == e)
         if not len(t):
@@ -350,14 +347,14 @@ def expected(x, gate, up, down, idx, wt, few):
     return y, tol
 
 
-def check_experts(y, x, gu, down, E, d, f, idx, wt, few):
-    want, tol = expected(host(x), *matrices(gu, down, E, d, f), idx.cpu().numpy(), host(wt), few)
+def check_experts(y, x, gu, down, E, d, f, idx, wt, telling=True):
+    want, tol = expected(host(x), *matrices(gu, down, E, d, f), idx.cpu().numpy(), host(wt))
     if y.dtype == torch.bfloat16:
         tol = tol + 2.0 ** -8 * (np.abs(want) + tol)
     err = np.abs(host(y) - want)
     assert (err <= tol + 1e-30).all(), float((err / np.maximum(tol, 1e-300)).max())
-    # the bound says something: most of it is far below the values (1440 and 3840 summands, all errors of one sign: a tenth)
-    assert np.median(tol) < 0.2 * np.sqrt(np.mean(want ** 2))
+    # the bound says something: most of it is below the values (1440 and 3840 summands, all errors of one sign: a tenth)
+    assert not telling or np.median(tol) < 0.2 * np.sqrt(np.mean(want ** 2))
 
 
 def routing(T, E, k, seed=0):
@@ -380,9 +377,50 @@ def test_experts(E, k, d, f, T, dtype):
     ex = P().Fp4Experts(d, f, E, k, gu, down, x_dtype=dtype, max_tokens=T + 3)
     y = ex.forward(x, idx, wt)
     assert ex.check() == 0
-    check_experts(y, x, gu, down, E, d, f, idx, wt, T <= 16)
+    check_experts(y, x, gu, down, E, d, f, idx, wt)
+    ex.ws.fill_(255)  # (nothing is kept there from one call to the next)
     assert torch.equal(y, ex.forward(x, idx, wt))
     ex.close()
+
+
+@pytest.mark.parametrize("T", [1, 3, 20])
+@pytest.mark.parametrize("d,f", [(64, 65536), (16384, 64), (5632, 32)])
+def test_experts_of_extreme_widths(d, f, T):
+    """Rows too long for a few-token call's shared memory go the way of many tokens."""
+    E, k = 2, 1
+    gu, down = make(E, d, f)
+    idx, wt = routing(T, E, k)
+    x = torch.randn(T, d, generator=torch.Generator().manual_seed(T)).bfloat16().cuda()
+    ex = P().Fp4Experts(d, f, E, k, gu, down, max_tokens=T)
+    y = ex.forward(x, idx, wt)
+    assert ex.check() == 0
+    check_experts(y, x, gu, down, E, d, f, idx, wt, telling=False)
+
+
+@pytest.mark.parametrize("rows", [5, 40])
+@pytest.mark.parametrize("n,N", [(21, 16), (65536, 24), (8, 8), (1000, 1000)])
+def test_product_of_odd_and_long_rows(rows, n, N):
+    g = torch.Generator().manual_seed(rows + n)
+    a, w = (P().fp4_quantize(torch.randn(r, n, generator=g).cuda()) for r in (rows, 2 * N))
+    offsets = [0, rows // 2, rows]
+    out = P().fp4_product(a, w, torch.tensor(offsets, dtype=torch.int32).cuda(), out_dtype=torch.float32)
+    check_product(a, w, offsets, 2, out)
+
+
+def test_a_token_with_an_infinity_spoils_itself_alone():
+    E, k, d, f = 4, 2, 128, 96
+    gu, down = make(E, d, f)
+    for T in (3, 40):
+        idx, wt = routing(T, E, k)
+        x = torch.randn(T, d, generator=torch.Generator().manual_seed(T)).bfloat16().cuda()
+        ex = P().Fp4Experts(d, f, E, k, gu, down, max_tokens=T)
+        y = ex.forward(x, idx, wt)
+        for bad in (float("inf"), float("nan")):
+            z = x.clone()
+            z[1, 70] = bad
+            got = ex.forward(z, idx, wt)
+            keep = torch.arange(T) != 1
+            assert got[1].isnan().all() and torch.equal(got[keep], y[keep])
 
 
 @pytest.mark.parametrize("T", [1, 5, 600])
@@ -392,7 +430,7 @@ def test_experts_at_the_paper_widths(T):
     idx, wt = routing(T, E, k)
     x = torch.randn(T, d, generator=torch.Generator().manual_seed(T)).bfloat16().cuda()
     ex = P().Fp4Experts(d, f, E, k, gu, down, max_tokens=T)
-    check_experts(ex.forward(x, idx, wt), x, gu, down, E, d, f, idx, wt, T <= 16)
+    check_experts(ex.forward(x, idx, wt), x, gu, down, E, d, f, idx, wt)
     assert ex.check() == 0
 
 
@@ -405,7 +443,7 @@ def test_uneven_routing_and_an_expert_named_twice(T):
     idx, wt = routing(T, E, k)
     for same in (idx * 0 + 5, idx * 0, idx // 2, torch.where(idx > 3, 7, 0).to(torch.int32)):
         y = ex.forward(x, same, wt)
-        check_experts(y, x, gu, down, E, d, f, same, wt, T <= 16)
+        check_experts(y, x, gu, down, E, d, f, same, wt)
     y = ex.forward(x, idx, wt * 0)
     assert not y.any()
     assert ex.check() == 0
@@ -422,7 +460,7 @@ def test_experts_out_of_range_are_reported_and_spoil_their_token_alone(T):
     for bad in (-1, E, 1 << 30):
         wrong = idx.clone()
         wrong[0, 1] = bad
-        ex.ws.zero_()
+        ex.ws.fill_(255)  # (whatever the workspace holds)
         z = ex.forward(x, wrong, wt)
         assert ex.check() == 6
         assert torch.equal(z[1:], y[1:])
@@ -479,7 +517,7 @@ def test_experts_captured_with_changing_inputs():
             torch.cuda.synchronize()
             got = y.clone()
             assert torch.equal(got, ex.forward(x, idx, wt))
-            check_experts(got, x, gu, down, E, d, f, idx, wt, T <= 16)
+            check_experts(got, x, gu, down, E, d, f, idx, wt)
         assert ex.check() == 0
 
 
@@ -521,7 +559,7 @@ def test_layer_with_4_bit_experts(T, rule):
     kw = dict(scoring="sigmoid", groups=4, kept=2, group_top=2, scale=2.5) if rule else {}
     want, ww = Q.select(host(lay.logits(x)), k, bias=None if bias is None else host(bias), **kw)
     assert np.array_equal(idx.cpu().numpy(), want) and np.allclose(w.cpu().numpy(), ww, rtol=1e-5)
-    check_experts(y, x, gu, down, E, d, f, idx, w, T <= 16)
+    check_experts(y, x, gu, down, E, d, f, idx, w)
     r = lay.route(x)
     assert torch.equal(r[0], idx) and torch.equal(r[1], w) and torch.equal(lay.fp4.forward(x, idx, w), y)
     out = torch.empty_like(y)
