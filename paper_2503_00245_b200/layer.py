@@ -35,7 +35,7 @@ class Fp4Rows:
     """A matrix in MXFP4: codes uint8 [rows, 16 ceil(n / 32)] and scales uint8 [ceil(n / 128), rows rounded up to 4, 4] (the layout of
     moe_fp4 in cosmoe.h)."""
 
-    __slots__ = ("codes", "scales", "rows", "n", "c")
+    __slots__ = ("_codes", "_scales", "_buf", "device", "rows", "n", "c")
 
     def __init__(self, codes, scales, n):
         rows, nb = codes.shape[0], -(-n // 32)
@@ -45,21 +45,49 @@ class Fp4Rows:
             raise ValueError(f"codes {tuple(codes.shape)} and scales {tuple(scales.shape)} are not those of {rows} rows of {n} values")
         if codes.device != scales.device:
             raise ValueError("codes and scales lie on different devices")
-        self.codes, self.scales, self.rows, self.n = codes, scales, rows, n
+        self._codes, self._scales, self._buf, self.device, self.rows, self.n = codes, scales, None, codes.device, rows, n
         self.c = B.make_fp4(codes, scales, rows, n)
 
     @classmethod
     def empty(cls, rows, n, device="cuda"):
+        return cls._over(torch.empty(cls._bytes(rows, n), dtype=torch.uint8, device=device), rows, n)
+
+    @staticmethod
+    def _bytes(rows, n):
         nb = -(-n // 32)
-        q = object.__new__(cls)  # (what it allocates itself needs no checks: they take longer than a small matrix)
-        q.codes = codes = torch.empty((rows, 16 * nb), dtype=torch.uint8, device=device)
-        q.scales = scales = torch.empty((-(-nb // 4), -(-rows // 4) * 4, 4), dtype=torch.uint8, device=device)
-        q.rows, q.n, q.c = rows, n, B.moe_fp4(codes.data_ptr(), scales.data_ptr(), rows, n)
+        return 16 * (rows * nb + -(-nb // 4) * -(-rows // 4))
+
+    @classmethod
+    def _over(cls, buf, rows, n):
+        """In one buffer, codes first; the two tensors are made when somebody asks for them (each takes as long as a small launch)."""
+        q = object.__new__(cls)
+        at = buf.data_ptr()
+        q._codes = q._scales = None
+        q._buf, q.device, q.rows, q.n = buf, buf.device, rows, n
+        q.c = B.moe_fp4(at, at + 16 * rows * -(-n // 32), rows, n)
         return q
+
+    @property
+    def codes(self):
+        if self._codes is None:
+            nb = -(-self.n // 32)
+            self._codes = self._buf[:16 * self.rows * nb].view(self.rows, 16 * nb)
+        return self._codes
+
+    @property
+    def scales(self):
+        if self._scales is None:
+            nb = -(-self.n // 32)
+            self._scales = self._buf[16 * self.rows * nb:].view(-(-nb // 4), -(-self.rows // 4) * 4, 4)
+        return self._scales
+
+    @property
+    def _tensor(self):
+        return self._codes if self._buf is None else self._buf
 
     def dequantize(self, dtype=torch.bfloat16):
         """The values, [rows, n] (n a multiple of 8)."""
-        out = torch.empty((self.rows, self.n), dtype=dtype, device=self.codes.device)
+        out = self._tensor.new_empty((self.rows, self.n), dtype=dtype)
         _here(out)
         B.moe_fp4_dequantize_rows(self.c, out)
         return out
@@ -83,7 +111,8 @@ def fp4_quantize(x, row_of=None, row_div=1):
             raise TypeError("row_of is a vector of int32")
         rows = row_of.shape[0]
     _here(x, row_of)
-    q = Fp4Rows.empty(rows, x.shape[1], x.device)
+    n = x.shape[1]
+    q = Fp4Rows._over(x.new_empty(Fp4Rows._bytes(rows, n), dtype=torch.uint8), rows, n)
     B.moe_fp4_quantize_rows(x, row_of, row_div, rows, q.c.codes, q.c.scales)
     return q
 
@@ -116,9 +145,9 @@ def fp4_product(a: Fp4Rows, w: Fp4Rows, expert_offsets, out=None, out_dtype=torc
     if expert_offsets.dtype != torch.int32 or E < 1:
         raise TypeError("expert_offsets is a vector of E + 1 int32")
     N = w.rows // E
-    _here(a.codes, w.codes, expert_offsets, out)
+    _here(a._tensor, w._tensor, expert_offsets, out)
     if out is None:
-        out = torch.empty((a.rows, N), dtype=out_dtype, device=a.codes.device)
+        out = expert_offsets.new_empty((a.rows, N), dtype=out_dtype)
         stride = N
     else:
         if tuple(out.shape) != (a.rows, N) or out.stride(1) != 1:
@@ -146,9 +175,9 @@ def select_experts(logits, rule: SelectRule, bias=None):
     if bias is not None and (bias.dtype != torch.float32 or bias.shape != (rule.E,)):
         raise ValueError(f"the bias has to be float32 [{rule.E}]")
     _here(logits, bias)
-    T, device = shape[0], logits.device
-    idx = torch.empty((T, rule.k), dtype=torch.int32, device=device)
-    w = torch.empty((T, rule.k), dtype=torch.float32, device=device)
+    T = shape[0]
+    idx = logits.new_empty((T, rule.k), dtype=torch.int32)
+    w = logits.new_empty((T, rule.k), dtype=torch.float32)
     B.moe_select(rule.c, logits, T, bias, idx, w, logits.stride(0) if T > 1 else rule.E)
     return idx, w
 
@@ -158,10 +187,10 @@ class Fp4Experts:
 
     def __init__(self, d_model, d_ff, n_experts, top_k, gu: Fp4Rows, down: Fp4Rows, x_dtype=torch.bfloat16, max_tokens=1, ctx=None):
         self.d, self.k, self.x_dtype, self.max_tokens = d_model, top_k, x_dtype, max_tokens
-        self.gu, self.down, self.device = gu, down, gu.codes.device
+        self.gu, self.down, self.device = gu, down, gu.device
         self.cfg = B.make_config(d_model, d_ff, n_experts, top_k, 0, B.MOE_F32 if x_dtype == torch.float32 else B.MOE_BF16)
         self.ctx, self.lent = ctx, ctx is not None  # (a layer lends its own)
-        _here(gu.codes, down.codes)
+        _here(gu._tensor, down._tensor)
         if ctx is None:
             self.ctx = B.moe_create(self.cfg)
         self.ws = torch.empty(B.moe_fp4_workspace_bytes(self.cfg, max_tokens), dtype=torch.uint8, device=self.device)
