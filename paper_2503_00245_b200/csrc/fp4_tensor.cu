@@ -7,16 +7,17 @@
 //
 // A pair of CTAs (cta_group::2) computes tiles of 256 rows x bn <= 192 columns: each CTA stages its 128 rows of A and half of the
 // tile's rows of W, 256 values (128 bytes, one swizzle row) of each at a time, and the words of scales (128 values each, csrc/fp4.cuh)
-// of its own rows and of ALL the tile's columns.  Four warps carry the words from shared to tensor memory, where the instruction wants
+// of its own rows and of ALL the tile's columns.  Warps carry the words from shared to tensor memory, where the instruction wants
 // them: word c of lane l is row 32 c + l's, the same in all four quarters of the lanes.  Tensor memory: two accumulators of 192
 // columns, so that a tile's epilogue runs under the next one's MMAs, and five stages of scales in the 128 columns left.  (bn = 256
 // would leave room for one accumulator.)
-// (Scales fetched by those warps straight from memory, three stages ahead: 50 us for 4096 rows x 2048 x 5632, 30 without the fetch.)
+// (4096 rows x 2048 x 5632 to bf16: 31 us.  Scales fetched by those warps straight from memory, three stages ahead: 50; by one set of
+// four warps instead of two in turn: 36.)
 // Roles in each CTA:
 //   warp 0      TMA producer: codes of A and W, both CTAs' on the leader's (rank 0) stage barrier; scales, on the CTA's own
 //   warp 1      allocates tensor memory; in the leader one lane issues the MMAs of both CTAs
-//   warps 2-5   scales, shared -> tensor memory (one warp per quarter of the lanes)
-//   warps 6-13  epilogue
+//   warps 2-9   scales, shared -> tensor memory (a warp for each quarter of the lanes, two sets that take the stages in turn)
+//   warps 10-17 epilogue
 // Tiles are handed out statically.  A tile may read rows of the next expert, or zeros; they are never stored.  All waits are
 // bounded; one that expires sets the ctx's status word.  No copy here is multicast.
 #include "fp4.cuh"
@@ -319,7 +320,7 @@ __global__ void __launch_bounds__(kThreads4, 1)
       }
     }
   } else {
-    // ================================================================= epilogue (warps 6..13, both CTAs)
+    // ================================================================= epilogue (warps 10..17, both CTAs)
     const int ew = warp - (2 + kScaleSets * kScaleWarps);
     const int q = warp & 3;
     const uint32_t acce_bar[2] = {map_to_rank(&sm.accum_empty[0], 0u), map_to_rank(&sm.accum_empty[1], 0u)};
