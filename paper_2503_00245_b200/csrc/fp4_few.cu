@@ -123,17 +123,20 @@ __device__ __forceinline__ bool epilogue_all(bool ok) {
 }
 
 // Whose rows this CTA takes, by warp 0: the CTAs are dealt out to the experts that have rows.
-__device__ __forceinline__ void few_find(const FewParams& P, FewSmem& sm, int lane, bool report) {
+template <int MODE>
+__device__ __forceinline__ void few_find(const FewParams& P, FewSmem& sm, int lane) {
   const unsigned FULL = 0xffffffffu;
   int pe[kFewRows / 32];
   unsigned m0 = 0u, m1 = 0u;
-  if (P.idx) {
+  if (MODE != FEW_OUT) {
 #pragma unroll
     for (int i = 0; i < kFewRows / 32; ++i) {
+      pe[i] = -1;
+      if (32 * i >= P.n) break;  // (what follows is not even fetched for a few pairs)
       const int p = lane + 32 * i;
       int e = p < P.n ? P.idx[p] : -1;
       if (p < P.n && (e < 0 || e >= P.E)) {
-        if (report) flag_error(P.st, MOE_ERR_STATE, 0x500u);
+        if (MODE == FEW_HIDDEN) flag_error(P.st, MOE_ERR_STATE, 0x500u);
         e = -1;
       }
       pe[i] = e;
@@ -154,18 +157,20 @@ __device__ __forceinline__ void few_find(const FewParams& P, FewSmem& sm, int la
     unsigned long long rest = mask;
     for (int i = 0; i < a; ++i) rest &= rest - 1;
     e = __ffsll((long long)rest) - 1;
-    if (P.idx) {
-      for (unsigned long long r = mask; r; r &= r - 1) {
+    if (MODE != FEW_OUT) {
+      // (DOWN: every expert's, for the number of parts that a block of y has)
+      for (unsigned long long r = MODE == FEW_DOWN ? mask : 1ull << e; r; r &= r - 1) {
         const int ee = __ffsll((long long)r) - 1;
         int have = 0;
 #pragma unroll
         for (int i = 0; i < kFewRows / 32; ++i) {
+          if (32 * i >= P.n) break;
           const unsigned is = __ballot_sync(FULL, pe[i] == ee);
           if (ee == e && pe[i] == ee) sm.rows[have + __popc(is & ((1u << lane) - 1u))] = lane + 32 * i;
           have += __popc(is);
         }
         if (ee == e) cnt = have;
-        expected += (have + P.tok_rows - 1) / P.tok_rows;
+        if (MODE == FEW_DOWN) expected += have <= P.tok_rows ? 1 : (have + P.tok_rows - 1) / P.tok_rows;
       }
     } else {
       const int lo = max(P.offsets[e], 0);
@@ -205,7 +210,7 @@ __global__ void __launch_bounds__(kFewThreads, 2)
   }
   // DOWN comes behind HIDDEN, which lets it start once it has itself waited for what was before: routing and matrix are there.
   if (MODE != FEW_DOWN) pdl_wait();
-  if (warp == 0) few_find(P, sm, lane, MODE == FEW_HIDDEN);
+  if (warp == 0) few_find<MODE>(P, sm, lane);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
