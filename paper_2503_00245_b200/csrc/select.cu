@@ -194,7 +194,7 @@ __device__ __forceinline__ unsigned groups_apart(const float* key, const moe_sel
 #pragma unroll 1
   for (int j = 0; j < c.groups_kept; ++j) {
     last = warp_max_f(mine);
-    const int win = __ffs(__ballot_sync(0xffffffffu, mine == last)) - 1;
+    const int win = max(__ffs(__ballot_sync(0xffffffffu, mine == last)) - 1, 0);  // (none: an infinite bias, decided in 64 bits)
     near = near || !(last > -CUDART_INF_F);
     kept |= 1u << (win / lanes);
     if (lane == win) mine = -CUDART_INF_F;

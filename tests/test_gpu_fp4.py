@@ -576,6 +576,36 @@ def test_layer_with_4_bit_experts(T, rule):
     lay.close()
 
 
+@pytest.mark.parametrize("T", [1, 7, 16, 24])
+def test_layers_one_after_the_other_in_a_graph(T):
+    """Kernels that start while the one ahead of them runs: a chain of layers, logits to sums, replayed on other inputs."""
+    E, k, d, f = 8, 2, 512, 384
+    g = torch.Generator().manual_seed(T)
+    lays = []
+    for i in range(3):
+        wr = (torch.randn(d, E, generator=g) * d ** -0.5).bfloat16().cuda()
+        rule = P().SelectRule(E, k, scoring="sigmoid", groups=4, groups_kept=2, group_top=2)
+        lays.append(P().MoELayer(d, f, E, k, wr, fp4=make(E, d, f, i), select=rule, select_bias=torch.zeros(E).cuda(), max_tokens=T))
+
+    def chain(x):
+        for lay in lays:
+            x = x + lay.forward(x)
+        return x
+    x = torch.randn(T, d, generator=g).bfloat16().cuda()
+    chain(x)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = chain(x)
+    for i in range(6):
+        x.copy_(torch.randn(T, d, generator=g).bfloat16())
+        for _ in range(3):
+            graph.replay()
+        torch.cuda.synchronize()
+        assert torch.isfinite(y).all() and torch.equal(y, chain(x))
+    assert all(lay.check() == 0 for lay in lays)
+
+
 @pytest.mark.parametrize("T", [1, 30])
 def test_dense_layer_with_a_selection_rule(T):
     from oracle import moe_oracle as O

@@ -114,6 +114,19 @@ def test_extreme_logits():
     assert run(l[2:3], None, k=2, scoring="sigmoid")[1].tolist() == [[0.0, 0.0]]
 
 
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+def test_infinite_and_large_biases(scoring):
+    """A bias of +inf puts an expert first, of -inf behind the others; keys of a large bias differ in bits that fp32 has not got."""
+    inf = float("inf")
+    l = logits(60, 48, seed=6)
+    bias = torch.randn(48, generator=torch.Generator().manual_seed(1)).mul(0.1)
+    bias[[5, 40]] = inf
+    bias[[7, 8, 30]] = -inf
+    check(l, bias.cuda(), k=8, scoring=scoring)
+    check(l, bias.cuda(), k=6, scoring=scoring, groups=6, kept=3, group_top=1)
+    check(l, torch.full((48,), 3e7).cuda() + torch.arange(48).cuda() % 3, k=8, scoring=scoring, groups=4, kept=2, group_top=2)
+
+
 def test_one_expert_and_no_tokens():
     check(logits(5, 1), None, k=1)
     check(logits(5, 1), torch.ones(1).cuda(), k=1, scoring="sigmoid", renorm=False)
