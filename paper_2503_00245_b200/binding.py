@@ -342,12 +342,14 @@ def make_fp4(codes, scales, rows, n) -> moe_fp4:
     return m
 
 
+_DTYPES = {torch.float32: MOE_F32, torch.bfloat16: MOE_BF16}
+
+
 def _dtype(t) -> int:
-    if t.dtype == torch.float32:
-        return MOE_F32
-    if t.dtype == torch.bfloat16:
-        return MOE_BF16
-    raise TypeError(f"float32 or bfloat16, not {t.dtype}")
+    d = _DTYPES.get(t.dtype)
+    if d is None:
+        raise TypeError(f"float32 or bfloat16, not {t.dtype}")
+    return d
 
 
 def moe_route_logits(ctx, x, T, w: moe_weights, logits, stream=None):

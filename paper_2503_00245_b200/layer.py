@@ -178,7 +178,7 @@ def select_experts(logits, rule: SelectRule, bias=None):
     T = shape[0]
     idx = logits.new_empty((T, rule.k), dtype=torch.int32)
     w = logits.new_empty((T, rule.k), dtype=torch.float32)
-    B.moe_select(rule.c, logits, T, bias, idx, w, logits.stride(0) if T > 1 else rule.E)
+    B.moe_select(rule.c, logits, T, bias, idx.data_ptr(), w.data_ptr(), logits.stride(0) if T > 1 else rule.E)
     return idx, w
 
 
