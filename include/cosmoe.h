@@ -226,7 +226,7 @@ int moe_fp4_experts(moe_ctx* ctx, const void* x, int32_t T, const moe_fp4* gu, c
  *    n_groups > 1: of the groups [g E / G, (g + 1) E / G) those groups_kept whose group_top (1 or 2) largest keys have the largest
  *    sum; experts of the others are out
  *    topk_idx[t][j] = the experts with the top_k largest keys, descending;   topk_w[t][j] = scale * s, divided by the sum of the
- *    chosen s when renorm (0 where that is 0)
+ *    chosen s when renorm (0 where that is 0); within 2^-20 of itself
  * Equal keys, and equal groups, go to the lower index.  Keys are formed and compared in 64 bits; where the order of the scores is
  * that of the logits (no bias, and no sums over groups) the logits are compared.  A logit of -inf switches an expert off: s = 0 and
  * it comes behind every other one (a token with nothing left gets the lowest experts, with weight 0); NaN counts as -inf; of +inf,

@@ -70,6 +70,12 @@ __device__ __forceinline__ float reciprocal(float v) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
   return r;
 }
+// e^(a - b), a <= b.  The difference is rounded, which would cost the power |a - b| 2^-24 of itself; what it lost (exact: two-sum) is
+// put back, so the power is as good as expf's (within 2.6 2^-24 of itself, measured over its arguments) and one product's.  0 below e^-104, where fp32 ends.
+__device__ __forceinline__ float exp_difference(float a, float b) {
+  const float d = a - b, minus_b = d - a, lost = (a - (d - minus_b)) - (b + minus_b), e = expf(d);
+  return d > -104.f ? fmaf(e, lost, e) : 0.f;
+}
 __device__ __forceinline__ unsigned f32_word(float v) { return f32_key(v == v ? v : -CUDART_INF_F); }
 __device__ __forceinline__ unsigned key_of(float v) { return f32_word(v); }
 __device__ __forceinline__ unsigned long long key_of(double v) { return f64_key(v); }
@@ -203,9 +209,10 @@ __device__ __forceinline__ unsigned groups_apart(const float* key, const moe_sel
   return kept;
 }
 
-// N: experts of a lane.  Warps go from token to token with the bias in registers.
+// N: experts of a lane.  Warps go from token to token with the bias in registers.  (Four blocks to an SM, 64 registers: with three,
+// 16384 tokens of 256 experts take 35 us in place of 30.)
 template <typename T, int N>
-__global__ void __launch_bounds__(kSelWarps * 32) select_kernel(const SelectParams P) {
+__global__ void __launch_bounds__(kSelWarps * 32, 4) select_kernel(const SelectParams P) {
   __shared__ unsigned long long s_key[kSelWarps][N * 32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const moe_select_config& c = P.c;
@@ -215,7 +222,7 @@ __global__ void __launch_bounds__(kSelWarps * 32) select_kernel(const SelectPara
   const unsigned inv_per = (65536u + per - 1) / per;  // (e inv_per >> 16 is e / per: e < 256, so the excess is below 1 / per)
   const bool softmax = c.scoring == MOE_SCORE_SOFTMAX;
   const bool by_logits = !P.bias && (G == 1 || c.group_top == 1);
-  const bool need_total = softmax && (!by_logits || !c.renorm);
+  const bool weight_total = softmax && !c.renorm;  // the total of a softmax divides the weights too
   pdl_launch_dependents();
   pdl_wait();
   float bias[N];
@@ -226,12 +233,13 @@ __global__ void __launch_bounds__(kSelWarps * 32) select_kernel(const SelectPara
     most = fmaxf(most, fabsf(bias[i]));
   }
   most = warp_max_f(most);
-  // Keys in 32 bits.  e^d = 2^(d log2 e) on the special-function unit: the exponent and its factor are rounded (1.25 2^-24 |d|), the
-  // power is within 2^-22 (PTX manual), so e^d is off by (1.25 |d| + 4) 2^-24 e^d, at most 5 2^-24 of 1 (|d| e^d <= 1 / e).  A sum of
-  // them in 13 steps: 18 2^-24 of itself; the quotient, with an approximate reciprocal (2^-23): 32 2^-24 of a score of at most 1.  A
-  // sigmoid: |l| e^-l / (1 + e^-l)^2 <= 1 / 2, below 16 2^-24.  Adding the bias rounds at 2^-24 of the sum, the expert's number in the
-  // low bits takes 16 2^-24, adding two keys rounds again.  So a key is known to 50 2^-24 (1 + |bias|), a sum of two to 102 2^-24;
-  // twice that is below the margin of 256 2^-24 (1 + |bias|).
+  // Keys in 32 bits.  e^d = 2^(d log2 e) on the special-function unit: d (a softmax's difference), the exponent and its factor are
+  // rounded (2.25 2^-24 |d|), the power is within 2^-22 (PTX manual), so e^d is off by (2.25 |d| + 4) 2^-24 e^d, at most 5 2^-24 of 1
+  // (|d| e^d <= 1 / e).  In a sum of E such terms the part that grows with |d| is 2.25 2^-24 of their mean |d|, which is at most ln E
+  // (5.6): with 4 2^-24 for the powers and 13 steps of addition, 30 2^-24 of itself; the quotient, with an approximate reciprocal
+  // (2^-23): 38 2^-24 of a score of at most 1.  A sigmoid: |l| e^-l / (1 + e^-l)^2 <= 1 / 2, below 16 2^-24.  Adding the bias rounds at
+  // 2^-24 of the sum, the expert's number in the low bits takes 16 2^-24, adding two keys rounds again.  So a key is known to 56
+  // 2^-24 (1 + |bias|), a sum of two to 114 2^-24; twice that is below the margin of 256 2^-24 (1 + |bias|).
   const float margin = by_logits ? -1.f : (1.f + most) * (256.f / 16777216.f);
 
 #pragma unroll 1
@@ -255,7 +263,15 @@ __global__ void __launch_bounds__(kSelWarps * 32) select_kernel(const SelectPara
     };
     float tot = 1.f;
     float s[N];
-    if (!by_logits || need_total) {
+    if (weight_total) {  // (to the weights' accuracy: terms within 4 2^-24 of themselves, added in 64 bits)
+      double part = 0.0;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        s[i] = l[i] == -CUDART_INF_F ? 0.f : l[i] == m ? 1.f : exp_difference(l[i], m);
+        part += (double)s[i];
+      }
+      tot = (float)warp_sum64(part);
+    } else if (!by_logits) {
       float part = 0.f;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
@@ -266,11 +282,9 @@ __global__ void __launch_bounds__(kSelWarps * 32) select_kernel(const SelectPara
         if (l[i] == -CUDART_INF_F) s[i] = 0.f;
         part += s[i];
       }
-      if (need_total) {
-        tot = warp_sum(part);
-        if (!(tot > 0.f)) tot = 1.f;
-      }
+      if (softmax) tot = warp_sum(part);
     }
+    if (!(tot > 0.f)) tot = 1.f;
     bool near = false;
     int my_e;
     if (by_logits) {  // (exact as they are)
@@ -340,10 +354,12 @@ __global__ void __launch_bounds__(kSelWarps * 32) select_kernel(const SelectPara
       }
       my_e = choose<unsigned long long, N>(wide, k, lane);
     }
-    // ---- weights: the chosen scores, in 32 bits where none of them is so small that 32 bits lose it
+    // ---- weights: the chosen scores, in 32 bits where none of them is so small that 32 bits lose it.  A score is within 4
+    // (softmax) or 5 (sigmoid) 2^-24 of itself; renormalised, with a sum of eight, a quotient and the factor, a weight is within 15
+    // 2^-24, else, with a total within 5, within 11.
     const float my_l = lane < k ? logit_or_off(row, my_e) : 0.f;
     float s32 = 0.f;
-    if (lane < k) s32 = my_l == -CUDART_INF_F ? 0.f : softmax ? (my_l == m ? 1.f : expf(my_l - m)) : 1.f / (1.f + expf(-my_l));
+    if (lane < k) s32 = my_l == -CUDART_INF_F ? 0.f : softmax ? (my_l == m ? 1.f : exp_difference(my_l, m)) : 1.f / (1.f + expf(-my_l));
     float w;
     if (__all_sync(0xffffffffu, lane >= k || s32 > 1e-30f)) {
       w = c.renorm ? s32 / warp_sum(s32) : s32 / tot;
