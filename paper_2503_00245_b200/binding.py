@@ -139,6 +139,12 @@ def _ptr(t) -> int | None:
     return t.data_ptr()
 
 
+def _strided(t) -> int:
+    """Like _ptr, for tensors whose strides are passed along."""
+    assert t.is_cuda or t.is_pinned(), "device-resident (or pinned host) tensors only"
+    return t.data_ptr()
+
+
 def _stream(stream=None) -> int:
     if stream is None:
         return _current_raw_stream(_current_device())
@@ -358,7 +364,7 @@ def moe_route_logits(ctx, x, T, w: moe_weights, logits, stream=None):
 
 def moe_select(cfg: moe_select_config, logits, T, bias, topk_idx, topk_w, stride=None, stream=None):
     """logits: rows `stride` values apart (n_experts by default), each contiguous."""
-    rc = _lib().moe_select(C.addressof(cfg), logits.data_ptr(), _dtype(logits), cfg.n_experts if stride is None else stride, T,
+    rc = _lib().moe_select(C.addressof(cfg), _strided(logits), _dtype(logits), cfg.n_experts if stride is None else stride, T,
                            None if bias is None else _ptr(bias), _ptr(topk_idx), _ptr(topk_w), _stream(stream))
     if rc:
         raise MoeError(rc, "moe_select")
@@ -372,7 +378,7 @@ def moe_fp4_bytes(rows: int, n: int):
 
 def moe_fp4_quantize_rows(src, row_of, row_div, rows, codes, scales, stream=None):
     """src [src_rows][n], any strides that are not negative."""
-    rc = _lib().moe_fp4_quantize_rows(src.data_ptr(), _dtype(src), src.shape[0], src.stride(0), src.stride(1),
+    rc = _lib().moe_fp4_quantize_rows(_strided(src), _dtype(src), src.shape[0], src.stride(0), src.stride(1),
                                       None if row_of is None else _ptr(row_of), row_div, rows, src.shape[1], _ptr(codes), _ptr(scales),
                                       _stream(stream))
     if rc:
@@ -380,7 +386,7 @@ def moe_fp4_quantize_rows(src, row_of, row_div, rows, codes, scales, stream=None
 
 
 def moe_fp4_dequantize_rows(m: moe_fp4, dst, row_stride=None, stream=None):
-    rc = _lib().moe_fp4_dequantize_rows(C.addressof(m), dst.data_ptr(), _dtype(dst), m.n if row_stride is None else row_stride,
+    rc = _lib().moe_fp4_dequantize_rows(C.addressof(m), _strided(dst), _dtype(dst), m.n if row_stride is None else row_stride,
                                         _stream(stream))
     if rc:
         raise MoeError(rc, "moe_fp4_dequantize_rows")
@@ -392,7 +398,7 @@ def moe_fp4_pack_dense(d, f, n_experts, w_gate, w_up, w_down, gu: moe_fp4, down:
 
 
 def moe_fp4_product(ctx, a: moe_fp4, w: moe_fp4, expert_offsets, n_experts, out, out_stride=None, stream=None):
-    rc = _lib().moe_fp4_product(ctx, C.addressof(a), C.addressof(w), _ptr(expert_offsets), n_experts, out.data_ptr(), _dtype(out),
+    rc = _lib().moe_fp4_product(ctx, C.addressof(a), C.addressof(w), _ptr(expert_offsets), n_experts, _strided(out), _dtype(out),
                                 w.rows // n_experts if out_stride is None else out_stride, _stream(stream))
     if rc:
         raise MoeError(rc, "moe_fp4_product")

@@ -1,0 +1,34 @@
+"""What the Python calls of selection and 4-bit rows refuse before anything reaches the library (no GPU needed)."""
+import pytest
+import torch
+
+
+class Unreached:
+    """Stands in for the library: a call that gets there has not been refused."""
+
+    def __getattr__(self, name):
+        def call(*args):
+            raise RuntimeError(f"{name} was called")
+        return call
+
+
+@pytest.fixture
+def B(monkeypatch):
+    from paper_2503_00245_b200 import binding
+    monkeypatch.setattr(binding, "_LIB", Unreached())
+    monkeypatch.setattr(binding, "_current_device", lambda: 0)
+    monkeypatch.setattr(binding, "_current_raw_stream", lambda device: 0)
+    return binding
+
+
+def test_tensors_in_pageable_host_memory(B):
+    """Strided ones among them: the binding passes their address to kernels."""
+    rows, out = torch.zeros(4, 64), torch.zeros(4, 8)
+    m = B.moe_fp4(1 << 20, 1 << 20, 4, 64)
+    for call in (lambda: B.moe_select(B.make_select_config(64, 2), rows, 4, None, 1 << 20, 1 << 20),
+                 lambda: B.moe_fp4_quantize_rows(rows, None, 1, 4, 1 << 20, 1 << 20),
+                 lambda: B.moe_fp4_quantize_rows(rows[:, ::2], None, 1, 4, 1 << 20, 1 << 20),
+                 lambda: B.moe_fp4_dequantize_rows(m, rows),
+                 lambda: B.moe_fp4_product(1 << 20, m, B.moe_fp4(1 << 20, 1 << 20, 8, 64), 1 << 20, 1, out)):
+        with pytest.raises(AssertionError):
+            call()
