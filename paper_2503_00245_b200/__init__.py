@@ -4,5 +4,5 @@
 a context and its workspace) that callers and the benchmark use.
 """
 from . import binding  # noqa: F401
-from .layer import (Fp4Experts, Fp4Rows, MoELayer, OffloadedStack, SelectRule, fp4_product, fp4_quantize,  # noqa: F401
-                    pack_dense, pack_fp4, pack_wd, select_experts)
+from .layer import (Fp4Experts, Fp4Rows, MoELayer, OffloadedStack, SelectRule, fp4_check, fp4_product,  # noqa: F401
+                    fp4_quantize, pack_dense, pack_fp4, pack_wd, select_experts)

@@ -136,11 +136,18 @@ def _shared_ctx():
     return _shared[here]
 
 
+def fp4_check() -> int:
+    """What moe_check says of the current device's calls of fp4_product that had no ctx: 0, or the first failure since the last check (an
+    expired wait: that call's output is undefined).  Waits for the current stream; what runs on others has to be waited for before."""
+    ctx = _shared.get(B._current_device())
+    return B.MOE_OK if ctx is None else B.moe_check(ctx)
+
+
 def fp4_product(a: Fp4Rows, w: Fp4Rows, expert_offsets, out=None, out_dtype=torch.bfloat16, ctx=None):
     """out[s] = a[s] times the matrix of the expert e with expert_offsets[e] <= s < expert_offsets[e + 1]; w holds the experts'
     matrices, w.rows / E rows each.  Rows outside the offsets are left as they are.  out: rows may lie apart.  Without a ctx (its
-    status word is what moe_check reads) the library's own for this device is used, made by the first call on it: let that one come
-    before a stream is captured."""
+    status word is what moe_check reads) the library's own for this device is used, whose status fp4_check() reads, made by the first
+    call on it: let that one come before a stream is captured."""
     E = expert_offsets.shape[0] - 1
     if expert_offsets.dtype != torch.int32 or E < 1:
         raise TypeError("expert_offsets is a vector of E + 1 int32")

@@ -32,3 +32,13 @@ def test_tensors_in_pageable_host_memory(B):
                  lambda: B.moe_fp4_product(1 << 20, m, B.moe_fp4(1 << 20, 1 << 20, 8, 64), 1 << 20, 1, out)):
         with pytest.raises(AssertionError):
             call()
+
+
+def test_failures_of_products_without_a_context_can_be_asked_for(B, monkeypatch):
+    import paper_2503_00245_b200 as P
+    monkeypatch.setattr(P.layer, "_shared", {0: 41, 1: 42})
+    asked = []
+    monkeypatch.setattr(B, "moe_check", lambda ctx: asked.append(ctx) or 5)
+    assert P.fp4_check() == 5 and asked == [41]
+    monkeypatch.setattr(B, "_current_device", lambda: 2)  # no call yet on this one
+    assert P.fp4_check() == 0 and asked == [41]
