@@ -4,6 +4,8 @@ No arithmetic of the layer happens here; every call forwards to libcosmoe.so.
 """
 from __future__ import annotations
 
+import threading
+
 import torch
 
 from . import binding as B
@@ -127,13 +129,18 @@ def pack_fp4(w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor):
 
 
 _shared = {}  # device index -> a ctx for calls that need no more of one than its status word
+_shared_lock = threading.Lock()
 
 
 def _shared_ctx():
     here = B._current_device()
-    if here not in _shared:
-        _shared[here] = B.moe_create(B.make_config(8, 8, 1, 1))
-    return _shared[here]
+    ctx = _shared.get(here)
+    if ctx is None:
+        with _shared_lock:  # (one for all threads: whose status fp4_check reads)
+            ctx = _shared.get(here)
+            if ctx is None:
+                ctx = _shared[here] = B.moe_create(B.make_config(8, 8, 1, 1))
+    return ctx
 
 
 def fp4_check() -> int:

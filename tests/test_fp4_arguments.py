@@ -42,3 +42,24 @@ def test_failures_of_products_without_a_context_can_be_asked_for(B, monkeypatch)
     assert P.fp4_check() == 5 and asked == [41]
     monkeypatch.setattr(B, "_current_device", lambda: 2)  # no call yet on this one
     assert P.fp4_check() == 0 and asked == [41]
+
+
+def test_threads_share_one_context(B, monkeypatch):
+    import threading
+    import time
+
+    from paper_2503_00245_b200 import layer as L
+    monkeypatch.setattr(L, "_shared", {})
+    made, got = [], []
+
+    def create(cfg):
+        time.sleep(0.05)  # (the other threads come while the first one's is being made)
+        made.append(len(made) + 1)
+        return made[-1]
+    monkeypatch.setattr(B, "moe_create", create)
+    threads = [threading.Thread(target=lambda: got.append(L._shared_ctx())) for _ in range(8)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert made == [1] and got == [1] * 8
