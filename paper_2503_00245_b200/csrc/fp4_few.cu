@@ -582,21 +582,19 @@ bool few_plan(const moe_ctx* ctx, int K, int n, FewPlan* plan) {
 }
 
 int few_maps(const moe_fp4* w, CUtensorMap* codes, CUtensorMap* scales) {
-  EncodeTiledFn fn = encode_fn();
-  if (!fn) return MOE_ERR_CUDA;
   const Fp4Shape sh = fp4_shape(w->rows, w->n);
   const cuuint32_t es[2] = {1, 1};
   {
     const cuuint64_t dims[2] = {(cuuint64_t)sh.pitch, (cuuint64_t)w->rows}, strides[1] = {(cuuint64_t)sh.pitch};
     const cuuint32_t box[2] = {128, kBlkRows};
-    if (fn(codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(w->codes), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    if (encode_tiled(codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, w->codes, dims, strides, box, es, CU_TENSOR_MAP_SWIZZLE_128B,
+                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B) != CUDA_SUCCESS)
       return MOE_ERR_CUDA;
   }
   const cuuint64_t dims[2] = {(cuuint64_t)sh.rp, (cuuint64_t)sh.chunks}, strides[1] = {(cuuint64_t)sh.rp * 4};
   const cuuint32_t box[2] = {kBlkRows, 4};
-  return fn(scales, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void*>(w->scales), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+  return encode_tiled(scales, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, w->scales, dims, strides, box, es, CU_TENSOR_MAP_SWIZZLE_NONE,
+                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B) == CUDA_SUCCESS
              ? MOE_OK
              : MOE_ERR_CUDA;
 }

@@ -401,14 +401,12 @@ __global__ void __launch_bounds__(kThreads4, 1)
 
 // rows of codes: box of 128 bytes x box_rows
 int make_map_codes(CUtensorMap* m, const void* base, long long rows, long long pitch, int box_rows) {
-  EncodeTiledFn fn = encode_fn();
-  if (!fn) return MOE_ERR_CUDA;
   const cuuint64_t dims[2] = {(cuuint64_t)pitch, (cuuint64_t)rows};
   const cuuint64_t strides[1] = {(cuuint64_t)pitch};
   const cuuint32_t box[2] = {128, (cuuint32_t)box_rows};
   const cuuint32_t es[2] = {1, 1};
-  const CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  const CUresult r = encode_tiled(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, base, dims, strides, box, es, CU_TENSOR_MAP_SWIZZLE_128B,
+                                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
   return r == CUDA_SUCCESS ? MOE_OK : MOE_ERR_CUDA;
 }
 
@@ -429,14 +427,12 @@ int pick_bn4(long long rows, int E, int N, int pairs, int step) {
 
 // words of scales [chunks][rp]: box of box_rows words x 2
 int make_map_scales(CUtensorMap* m, const void* base, const Fp4Shape& sh, int box_rows) {
-  EncodeTiledFn fn = encode_fn();
-  if (!fn) return MOE_ERR_CUDA;
   const cuuint64_t dims[2] = {(cuuint64_t)sh.rp, (cuuint64_t)sh.chunks};
   const cuuint64_t strides[1] = {(cuuint64_t)sh.rp * 4};
   const cuuint32_t box[2] = {(cuuint32_t)box_rows, 2};
   const cuuint32_t es[2] = {1, 1};
-  const CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                        CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  const CUresult r = encode_tiled(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, base, dims, strides, box, es, CU_TENSOR_MAP_SWIZZLE_NONE,
+                                  CU_TENSOR_MAP_L2_PROMOTION_L2_128B);
   return r == CUDA_SUCCESS ? MOE_OK : MOE_ERR_CUDA;
 }
 
