@@ -64,7 +64,7 @@ struct moe_ctx {
   cosmoe::DeviceState* h_state;  // pinned host mirror for moe_check
   long long* acc;                // device: fixed-point output accumulators of the dense streaming path, kept zero
   size_t acc_elems;              //         between calls by the kernel itself (MOE_STREAM_MAX_TOKENS*top_k*d)
-  unsigned long long launches;
+  std::atomic<unsigned long long> launches;  // (some calls on one ctx may overlap)
   std::atomic<unsigned long long>* smem_ok;  // kernels that may use all the shared memory of a CTA, a bit each (allow_full_smem)
   std::atomic<unsigned long long> smem_ok_own;
   long long fin_wait_budget;     // cycles the dense streaming kernel's finalisers wait for the arrival counter (0 = default)

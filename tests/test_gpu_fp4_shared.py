@@ -81,3 +81,29 @@ def test_layers_are_a_threads_first_calls(rank, fp4, T):
         in_a_thread(lambda: lay.fp4.forward(t["x"], idx, wt, y))
         torch.cuda.synchronize()
         assert torch.equal(y, want)
+
+
+def test_threads_on_one_context_count_every_launch():
+    """Products on one context may overlap, so may their host sides (a call through ctypes runs without the interpreter's lock)."""
+    import threading
+
+    import paper_2503_00245_b200 as P
+    from paper_2503_00245_b200 import binding as B
+    a, w, at = rows(1, 64, 1), rows(8, 64, 2), torch.tensor([0, 1], dtype=torch.int32).cuda()
+    want = P.fp4_product(a, w, at)
+    ctx = B.moe_create(B.make_config(8, 8, 1, 1))
+    threads, calls = 8, 2000
+    outs = [torch.zeros(1, 8, dtype=torch.bfloat16).cuda() for _ in range(threads)]
+
+    def work(i):
+        for _ in range(calls):
+            P.fp4_product(a, w, at, out=outs[i], ctx=ctx)
+    before = B.moe_launch_count(ctx)
+    pool = [threading.Thread(target=work, args=(i,)) for i in range(threads)]
+    for t in pool:
+        t.start()
+    for t in pool:
+        t.join()
+    assert B.moe_launch_count(ctx) - before == threads * calls
+    assert B.moe_check(ctx) == 0 and all(torch.equal(o, want) for o in outs)
+    B.moe_destroy(ctx)
