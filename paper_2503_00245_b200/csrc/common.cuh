@@ -76,9 +76,10 @@ namespace cosmoe {
 // front of every launch.  (The limit only permits; a launch still takes what it asks for.  It is an attribute of the function
 // in one CUDA context, as a ctx's memory belongs to one: a device may have several.)
 constexpr int kMaxDevices = 64;
-inline unsigned long long next_smem_bit() {  // (at most 64 kernels ask)
+inline unsigned long long next_smem_bit() {  // (0 behind 64 kernels: the limit is then set in front of every launch)
   static std::atomic<unsigned> n{0};
-  return 1ull << n.fetch_add(1);
+  const unsigned i = n.fetch_add(1);
+  return i < 64 ? 1ull << i : 0ull;
 }
 template <auto Kernel>
 int allow_full_smem(const moe_ctx* ctx) {

@@ -27,3 +27,10 @@ def test_launches_of_overlapping_calls_are_all_counted(tmp_path):
   for (auto& t : pool) t.join();
   printf("%llu", (unsigned long long)ctx.launches);""")
     assert out == ["4000000"]
+
+
+@pytest.mark.skipif(not os.path.exists(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")), reason="needs nvcc")
+def test_kernels_beyond_the_mask_of_shared_memory_limits_have_no_bit(tmp_path):
+    """(allow_full_smem asks the driver again for each of their launches; with another kernel's bit it would never ask.)"""
+    bits = [int(v) for v in run(tmp_path, '  for (int i = 0; i < 70; ++i) printf("%llu ", cosmoe::next_smem_bit());')]
+    assert bits[:64] == [1 << i for i in range(64)] and bits[64:] == [0] * 6
