@@ -244,19 +244,26 @@ class Fp4Experts:
 class MoELayer:
     """One MoE layer's packed weights plus a context and workspace sized for up to max_tokens.
 
-    Experts: dense (pack_dense), wd (pack_wd) or fp4 (pack_fp4).  select: a SelectRule that chooses the experts from the router's
-    logits, with select_bias seen by the selection alone, in place of the paper's softmax and top-k."""
+    Experts: dense (pack_dense), wd (pack_wd) or fp4 (pack_fp4).  renorm (True): a token's weights are rescaled to sum to 1.  select: a
+    SelectRule that chooses the experts from the router's logits, with select_bias seen by the selection alone, in place of the paper's
+    softmax and top-k; whether weights are rescaled is then the rule's to say."""
 
     by_steps, select, fp4, ctx = False, None, None, None
 
     def __init__(self, d_model, d_ff, n_experts, top_k, w_router, b_router=None, *, dense=None, wd=None, fp4=None,
-                 x_dtype=torch.bfloat16, renorm=True, path=B.MOE_PATH_AUTO, max_tokens=1, expert_slot=None, select=None,
+                 x_dtype=torch.bfloat16, renorm=None, path=B.MOE_PATH_AUTO, max_tokens=1, expert_slot=None, select=None,
                  select_bias=None):
         assert (dense is not None) + (wd is not None) + (fp4 is not None) == 1
         if select is not None and (select.E, select.k) != (n_experts, top_k):
             raise ValueError("the selection rule is for other numbers of experts")
         if select is None and select_bias is not None:
             raise ValueError("select_bias without a selection rule")
+        if select is not None:
+            if renorm is not None and bool(renorm) != bool(select.c.renorm):
+                raise ValueError(f"renorm={renorm}, but the selection rule, which makes the weights, has renorm={bool(select.c.renorm)}")
+            renorm = select.c.renorm
+        elif renorm is None:
+            renorm = True
         if fp4 is not None and (path != B.MOE_PATH_AUTO or expert_slot is not None):
             raise ValueError("4-bit experts take neither a path nor expert_slot")
         self.select, self.select_bias = select, select_bias

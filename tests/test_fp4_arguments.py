@@ -63,3 +63,23 @@ def test_threads_share_one_context(B, monkeypatch):
     for t in threads:
         t.join()
     assert made == [1] and got == [1] * 8
+
+
+@pytest.mark.parametrize("layers,rules,fits", [(None, True, True), (None, False, True), (True, True, True), (False, False, True),
+                                               (False, True, False), (True, False, False)])
+def test_a_layers_renorm_agrees_with_its_rule(B, monkeypatch, layers, rules, fits):
+    import paper_2503_00245_b200 as P
+    monkeypatch.setattr(B, "make_weights", lambda *a, **k: None)
+    monkeypatch.setattr(B, "moe_create", lambda cfg: 41)
+    monkeypatch.setattr(B, "moe_destroy", lambda ctx: None)
+    monkeypatch.setattr(B, "moe_workspace_bytes", lambda cfg, T: 16)
+    kw = dict(dense=torch.zeros(1), select=P.SelectRule(8, 2, renorm=rules))
+    if layers is not None:
+        kw["renorm"] = layers
+    if not fits:
+        with pytest.raises(ValueError):
+            P.MoELayer(64, 64, 8, 2, torch.zeros(64, 8), **kw)
+        return
+    assert P.MoELayer(64, 64, 8, 2, torch.zeros(64, 8), **kw).cfg.renorm == rules
+    del kw["select"]  # without a rule: as asked, True where nothing is
+    assert P.MoELayer(64, 64, 8, 2, torch.zeros(64, 8), **kw).cfg.renorm == (layers is not False)
