@@ -404,7 +404,7 @@ extern "C" int moe_select(const moe_select_config* cfg, const void* logits, int3
   if ((uintptr_t)logits % (dtype == MOE_F32 ? 4 : 2) || ((uintptr_t)bias | (uintptr_t)topk_idx | (uintptr_t)topk_w) & 3u) return MOE_ERR_INVALID_ARG;
   const SelectParams P{c, logits, stride, bias, T, topk_idx, topk_w};
   // (a few tokens for each warp where there are many: 148 SMs hold about 600 of these blocks)
-  const dim3 grid(std::min((T + kSelWarps - 1) / kSelWarps, 592)), block(kSelWarps * 32);
+  const dim3 grid(std::min((T - 1) / kSelWarps + 1, 592)), block(kSelWarps * 32);
   cudaStream_t s = (cudaStream_t)stream;
 #define SELECT(N)                                                              \
   MOE_CUDA_TRY(dtype == MOE_F32 ? launch_pdl(select_kernel<float, N>, grid, block, 0, s, P) \

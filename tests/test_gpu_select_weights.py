@@ -65,3 +65,20 @@ def test_totals_of_many_equal_terms():
     l[:, 17] = torch.rand(200, generator=g) + 0.1
     check(l.cuda(), None, k=4, renorm=False)
     check(l.cuda(), torch.zeros(256).cuda(), k=4, renorm=False)
+
+
+def test_as_many_tokens_as_a_call_can_name():
+    """2^31 - 1 of them (22 GB in all): the number of blocks comes out of a division that must not pass 32 bits before it."""
+    import paper_2503_00245_b200 as P
+    T = 2 ** 31 - 1
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB")
+    l = torch.zeros(T, 1, dtype=torch.bfloat16, device="cuda")
+    l[T - 1] = 1.0
+    idx, w = P.select_experts(l, P.SelectRule(1, 1, scoring="sigmoid", renorm=False))
+    assert not idx.any()
+    for part in w[: T - 1].split(1 << 28):
+        assert (part == 0.5).all()
+    assert abs(float(w[T - 1]) - 1 / (1 + np.exp(-1.0))) < RTOL
+    del l, idx, w, part
+    torch.cuda.empty_cache()
