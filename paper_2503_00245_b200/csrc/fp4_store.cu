@@ -225,22 +225,26 @@ int quantize_t(const Fp4Source& q, long long rows, int n, void* codes, void* sca
 
 // ---- rows of many tokens on their way to their experts: grouping and quantisation in one launch
 // Pairs (token, choice) are numbered in order; a pair's slot is its expert's first slot plus the number of earlier pairs of that expert.
-// Every CTA counts the pairs of all tokens by expert, those in front of its own tokens apart (n words from L2), ranks its own, and writes each of its tokens' rows, quantised once, to the token's k slots.  So no CTA waits
-// for another and nothing is left to clear.  (A grouping launch of one CTA and a gathering one: 18 us for 2048 tokens, two experts each.)
+// Every CTA counts the pairs of all tokens by expert (n words from L2), those in front of its own tokens apart, ranks its own, and
+// writes each of its tokens' rows, quantised once, to the token's k slots.  So no CTA waits for another and nothing is left to clear.
+// There are two CTAs to an SM at most, whatever the number of tokens, as each walks all pairs: with 1024 tokens to a CTA and the more
+// CTAs, the time went with the square (d 8, f 8, 8 of 8 experts: a call of a million tokens 9 ms, of four million 88, now 6 and 26).
+// (A grouping launch of one CTA and a gathering one: 18 us for 2048 tokens, two
+// experts each.)
 constexpr int kPlaceWarps = 8;
 struct PlaceParams {
   const void* x;
   const int32_t* idx;
-  int T, k, E, d, tokens;  // tokens of a CTA
+  int T, k, E, d, tokens, piece;  // tokens of a CTA, and of those whose slots it holds at a time
   int32_t *offsets, *inv;
   unsigned char* codes;
   uint32_t* scales;
   Fp4Shape sh;
   DeviceState* st;
 };
-template <typename T>
+template <typename T, bool kPieces>  // (kPieces: more of them than one.  A loop in all launches cost those of one piece 0.5 us)
 __global__ void __launch_bounds__(kPlaceWarps * 32) fp4_place_kernel(const PlaceParams P) {
-  extern __shared__ int s_slot[];  // [tokens][k]
+  extern __shared__ int s_slot[];  // [piece][k]
   __shared__ int s_all[kPlaceWarps][MOE_MAX_EXPERTS], s_before[kPlaceWarps][MOE_MAX_EXPERTS], s_next[MOE_MAX_EXPERTS];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_launch_dependents();
@@ -253,18 +257,18 @@ __global__ void __launch_bounds__(kPlaceWarps * 32) fp4_place_kernel(const Place
     return e >= 0 && e < P.E ? e : -1;
   };
   // ---- the warp's first row is on its way while the pairs are counted
-  const int parts = (P.d + 256 * kFly - 1) / (256 * kFly), tasks = (t1 - t0) * parts;
+  const int parts = (P.d + 256 * kFly - 1) / (256 * kFly);
   typename EightOf<T>::type f[kFly];
-  auto fetch = [&](int i) {
+  auto fetch = [&](int from, int i) {
     const int t = i / parts, c0 = (i - t * parts) * 256 * kFly + lane * 8;
-    const T* row = (const T*)P.x + (long long)(t0 + t) * P.d;
+    const T* row = (const T*)P.x + (long long)(from + t) * P.d;
 #pragma unroll
     for (int u = 0; u < kFly; ++u) {
       f[u] = {};
       if (c0 + 256 * u < P.d) f[u] = load8(row + c0 + 256 * u);
     }
   };
-  if (warp < tasks) fetch(warp);
+  if (warp < ((kPieces ? min(t0 + P.piece, t1) : t1) - t0) * parts) fetch(t0, warp);
   // ---- counts, by the warps' own counters; eight loads on their way
   const unsigned below = (1u << lane) - 1u;
   constexpr int kPairs = 8;
@@ -300,35 +304,45 @@ __global__ void __launch_bounds__(kPlaceWarps * 32) fp4_place_kernel(const Place
       if (lane == 0) P.offsets[P.E] = total;
     }
     __syncwarp();
-    // ---- slots of the CTA's own pairs, in order
-    const int mine = (t1 - t0) * P.k;
-    for (int p0 = 0; p0 < mine; p0 += 32) {
-      const int p = p0 + lane, e = p < mine ? expert(own + p) : -1;
-      if (p < mine && e < 0) flag_error(P.st, MOE_ERR_STATE, 0x530u);
-      const unsigned peers = __match_any_sync(0xffffffffu, e);
-      const int slot = e >= 0 ? s_next[e] + __popc(peers & below) : -1;
-      __syncwarp();
-      if (e >= 0 && (peers & below) == 0u) s_next[e] += __popc(peers);
-      __syncwarp();
-      if (p < mine) s_slot[p] = slot, P.inv[own + p] = max(slot, 0);  // (a pair without an expert: any slot, its token is undefined)
-    }
   }
-  __syncthreads();
-  // ---- the rows: a warp for 1024 values of a token
-  for (int i = warp; i < tasks; i += kPlaceWarps) {
-    const int t = i / parts, c0 = (i - t * parts) * 256 * kFly + lane * 8;
-    if (i != warp) fetch(i);
-#pragma unroll
-    for (int u = 0; u < kFly; ++u) {
-      const int c = c0 + 256 * u;
-      if (c - lane * 8 >= P.d) break;
-      uint32_t word, scale;
-      quantize_step(f[u], c, lane, P.sh, word, scale);
-      for (int j = 0; j < P.k; ++j) {
-        const int slot = s_slot[t * P.k + j];
-        if (slot >= 0) store_step(word, scale, c, slot, P.d, lane, P.codes, P.scales, P.sh);
+  for (int from = t0;;) {
+    const int to = kPieces ? min(from + P.piece, t1) : t1;
+    if (warp == 0) {
+      // ---- slots of the CTA's own pairs, in order
+      const int mine = (to - from) * P.k, first = from * P.k;
+      for (int p0 = 0; p0 < mine; p0 += 32) {
+        const int p = p0 + lane, e = p < mine ? expert(first + p) : -1;
+        if (p < mine && e < 0) flag_error(P.st, MOE_ERR_STATE, 0x530u);
+        const unsigned peers = __match_any_sync(0xffffffffu, e);
+        const int slot = e >= 0 ? s_next[e] + __popc(peers & below) : -1;
+        __syncwarp();
+        if (e >= 0 && (peers & below) == 0u) s_next[e] += __popc(peers);
+        __syncwarp();
+        // (a pair without an expert: any slot, its token is undefined)
+        if (p < mine) s_slot[p] = slot, P.inv[first + p] = max(slot, 0);
       }
     }
+    __syncthreads();
+    // ---- the rows: a warp for 1024 values of a token
+    const int tasks = (to - from) * parts;
+    for (int i = warp; i < tasks; i += kPlaceWarps) {
+      const int t = i / parts, c0 = (i - t * parts) * 256 * kFly + lane * 8;
+      if ((kPieces && from != t0) || i != warp) fetch(from, i);
+#pragma unroll
+      for (int u = 0; u < kFly; ++u) {
+        const int c = c0 + 256 * u;
+        if (c - lane * 8 >= P.d) break;
+        uint32_t word, scale;
+        quantize_step(f[u], c, lane, P.sh, word, scale);
+        for (int j = 0; j < P.k; ++j) {
+          const int slot = s_slot[t * P.k + j];
+          if (slot >= 0) store_step(word, scale, c, slot, P.d, lane, P.codes, P.scales, P.sh);
+        }
+      }
+    }
+    if (!kPieces || to == t1) break;
+    __syncthreads();
+    from = to;
   }
 }
 
@@ -345,16 +359,15 @@ int launch_fp4_quantize(const Fp4Source& src, long long rows, int n, void* codes
 int launch_fp4_place(moe_ctx* ctx, const void* x, const int32_t* idx, int T, int32_t* offsets, int32_t* inv, void* codes, void* scales,
                      cudaStream_t s) {
   const moe_config& c = ctx->cfg;
-  PlaceParams P{x, idx, T, c.top_k, c.n_experts, c.d_model, 0, offsets, inv, (unsigned char*)codes, (uint32_t*)scales,
+  PlaceParams P{x, idx, T, c.top_k, c.n_experts, c.d_model, 0, 0, offsets, inv, (unsigned char*)codes, (uint32_t*)scales,
                 fp4_shape((long long)T * c.top_k, c.d_model), ctx->d_state};
-  // two CTAs to an SM, or more tokens each where there are many
-  P.tokens = std::max(2, std::min((T + 2 * ctx->sm_count - 1) / (2 * ctx->sm_count), 1024));
-  const dim3 grid((unsigned)((T + P.tokens - 1) / P.tokens)), block(kPlaceWarps * 32);
-  const size_t smem = (size_t)P.tokens * c.top_k * 4;
-  if (c.x_dtype == MOE_F32)
-    MOE_CUDA_TRY(launch_pdl(fp4_place_kernel<float>, grid, block, smem, s, P));
-  else
-    MOE_CUDA_TRY(launch_pdl(fp4_place_kernel<__nv_bfloat16>, grid, block, smem, s, P));
+  P.tokens = std::max(2, (T - 1) / (2 * ctx->sm_count) + 1), P.piece = std::min(P.tokens, 1024);
+  const dim3 grid((unsigned)((T - 1) / P.tokens + 1)), block(kPlaceWarps * 32);
+  const size_t smem = (size_t)P.piece * c.top_k * 4;
+  const bool pieces = P.piece < P.tokens;
+  MOE_CUDA_TRY(launch_pdl(c.x_dtype == MOE_F32 ? (pieces ? fp4_place_kernel<float, true> : fp4_place_kernel<float, false>)
+                                               : (pieces ? fp4_place_kernel<__nv_bfloat16, true> : fp4_place_kernel<__nv_bfloat16, false>),
+                          grid, block, smem, s, P));
   ctx->launches++;
   return MOE_OK;
 }
