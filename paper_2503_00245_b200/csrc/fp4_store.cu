@@ -229,8 +229,7 @@ int quantize_t(const Fp4Source& q, long long rows, int n, void* codes, void* sca
 // writes each of its tokens' rows, quantised once, to the token's k slots.  So no CTA waits for another and nothing is left to clear.
 // There are two CTAs to an SM at most, whatever the number of tokens, as each walks all pairs: with 1024 tokens to a CTA and the more
 // CTAs, the time went with the square (d 8, f 8, 8 of 8 experts: a call of a million tokens 9 ms, of four million 88, now 6 and 26).
-// (A grouping launch of one CTA and a gathering one: 18 us for 2048 tokens, two
-// experts each.)
+// (A grouping launch of one CTA and a gathering one: 18 us for 2048 tokens, two experts each.)
 constexpr int kPlaceWarps = 8;
 struct PlaceParams {
   const void* x;

@@ -122,6 +122,10 @@ def fp4_quantize(x, row_of=None, row_div=1):
 def pack_fp4(w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor):
     """[E,d,f], [E,d,f], [E,f,d] bf16 (maths layout) -> the experts in MXFP4: (gu, down)."""
     E, d, f = w_gate.shape
+    if any(w.dtype != torch.bfloat16 for w in (w_gate, w_up, w_down)):
+        raise TypeError("the experts' matrices are bfloat16")
+    if w_up.shape != (E, d, f) or w_down.shape != (E, f, d):
+        raise ValueError(f"w_gate {tuple(w_gate.shape)}, w_up {tuple(w_up.shape)} and w_down {tuple(w_down.shape)} are not [E,d,f], [E,d,f] and [E,f,d]")
     _here(w_gate, w_up, w_down)
     gu, down = Fp4Rows.empty(E * 64 * -(-f // 32), d, w_gate.device), Fp4Rows.empty(E * d, f, w_gate.device)
     B.moe_fp4_pack_dense(d, f, E, w_gate, w_up, w_down, gu.c, down.c)

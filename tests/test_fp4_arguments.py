@@ -83,3 +83,23 @@ def test_a_layers_renorm_agrees_with_its_rule(B, monkeypatch, layers, rules, fit
     assert P.MoELayer(64, 64, 8, 2, torch.zeros(64, 8), **kw).cfg.renorm == rules
     del kw["select"]  # without a rule: as asked, True where nothing is
     assert P.MoELayer(64, 64, 8, 2, torch.zeros(64, 8), **kw).cfg.renorm == (layers is not False)
+
+
+def test_experts_to_be_packed_have_fitting_shapes_and_types(B, monkeypatch):
+    """The library is given three addresses and one set of sizes: a smaller matrix would be read behind its end."""
+    import paper_2503_00245_b200 as P
+    monkeypatch.setattr(P.layer, "_here", lambda *t: None)
+    packed = []
+    monkeypatch.setattr(B, "moe_fp4_pack_dense", lambda *a: packed.append(a[:3]))
+    w = [torch.zeros(2, 64, 40, dtype=torch.bfloat16), torch.zeros(2, 64, 40, dtype=torch.bfloat16), torch.zeros(2, 40, 64, dtype=torch.bfloat16)]
+    P.pack_fp4(*w)
+    assert packed == [(64, 40, 2)]
+    for i, bad in ((1, w[1][:1]), (1, w[1][:, :32]), (1, w[2]), (2, w[2][:, :32]), (2, w[1]), (2, w[2][0])):
+        with pytest.raises(ValueError):
+            P.pack_fp4(*w[:i], bad, *w[i + 1:])
+    for i in range(3):
+        with pytest.raises(TypeError):
+            P.pack_fp4(*w[:i], w[i].float(), *w[i + 1:])
+        with pytest.raises(TypeError):
+            P.pack_fp4(*w[:i], w[i].half(), *w[i + 1:])
+    assert len(packed) == 1
