@@ -308,6 +308,10 @@ class MoELayer:
 
     # ---- step-by-step calls -------------------------------------------------------------
     def logits(self, x):
+        """x [T, d] -> the router's logits, float32 [T, E]."""
+        if x.dim() != 2 or x.shape[1] != self.d or x.dtype != self.x_dtype:
+            raise ValueError(f"x has to be {self.x_dtype} [T, {self.d}]")
+        _here(x)
         out = torch.empty((x.shape[0], self.E), dtype=torch.float32, device=self.device)
         B.moe_route_logits(self.ctx, x, x.shape[0], self.weights, out)
         return out

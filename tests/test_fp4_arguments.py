@@ -103,3 +103,28 @@ def test_experts_to_be_packed_have_fitting_shapes_and_types(B, monkeypatch):
         with pytest.raises(TypeError):
             P.pack_fp4(*w[:i], w[i].half(), *w[i + 1:])
     assert len(packed) == 1
+
+
+@pytest.fixture
+def layer(B, monkeypatch):
+    """A layer with a selection rule whose library calls are noted and not made."""
+    import paper_2503_00245_b200 as P
+    monkeypatch.setattr(P.layer, "_here", lambda *t: None)
+    monkeypatch.setattr(B, "make_weights", lambda *a, **k: None)
+    monkeypatch.setattr(B, "moe_create", lambda cfg: 41)
+    monkeypatch.setattr(B, "moe_destroy", lambda ctx: None)
+    monkeypatch.setattr(B, "moe_workspace_bytes", lambda cfg, T: 16)
+    lay = P.MoELayer(64, 64, 8, 2, torch.zeros(64, 8), dense=torch.zeros(1), select=P.SelectRule(8, 2), max_tokens=4)
+    lay.asked = []
+    monkeypatch.setattr(B, "moe_route_logits", lambda ctx, x, T, w, out: lay.asked.append((T, tuple(out.shape))))
+    return lay
+
+
+def test_rows_whose_logits_are_asked_for_have_the_layers_width_and_type(layer):
+    x = torch.zeros(3, 64, dtype=torch.bfloat16)
+    layer.logits(x)
+    for bad in (x[:, :56], torch.zeros(3, 72, dtype=torch.bfloat16), x.float(), x.half(), x[0], x[None]):
+        for call in (layer.logits, layer.route, layer.forward):
+            with pytest.raises(ValueError):
+                call(bad)
+    assert layer.asked == [(3, (3, 8))]
