@@ -222,7 +222,7 @@ class Fp4Experts:
             raise ValueError(f"x has to be {self.x_dtype} [T, {self.d}]")
         if topk_idx.shape != (T, self.k) or topk_w.shape != (T, self.k) or topk_idx.dtype != torch.int32 or topk_w.dtype != torch.float32:
             raise ValueError(f"the routing has to be int32 and float32 [{T}, {self.k}]")
-        _here(x, topk_idx, topk_w, self.ws)
+        _here(x, topk_idx, topk_w, y, self.ws)
         if y is None:
             y = torch.empty((T, self.d), dtype=self.x_dtype, device=self.device)
         elif y.shape != (T, self.d) or y.dtype != self.x_dtype:

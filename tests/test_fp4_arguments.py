@@ -128,3 +128,29 @@ def test_rows_whose_logits_are_asked_for_have_the_layers_width_and_type(layer):
             with pytest.raises(ValueError):
                 call(bad)
     assert layer.asked == [(3, (3, 8))]
+
+
+def test_experts_outputs_lie_on_the_current_device(B, monkeypatch):
+    import paper_2503_00245_b200 as P
+
+    class Tensor(torch.Tensor):
+        index = 0
+
+        def get_device(self):
+            return self.index
+
+    def made(*shape, dtype=torch.bfloat16):
+        return torch.zeros(*shape, dtype=dtype).as_subclass(Tensor)
+    ex = object.__new__(P.Fp4Experts)
+    ex.d, ex.k, ex.x_dtype, ex.max_tokens, ex.device, ex.ctx, ex.lent = 64, 2, torch.bfloat16, 4, torch.device("cpu"), 41, True
+    ex.ws, ex.gu, ex.down = made(16), P.Fp4Rows.empty(0, 64, "cpu"), P.Fp4Rows.empty(0, 64, "cpu")
+    ran = []
+    monkeypatch.setattr(B, "moe_fp4_experts", lambda *a: ran.append(a))
+    x, idx, wt, y = made(3, 64), made(3, 2, dtype=torch.int32), made(3, 2, dtype=torch.float32), made(3, 64)
+    assert ex.forward(x, idx, wt, y) is y and len(ran) == 1
+    for t in (x, idx, wt, y):
+        t.index = 1
+        with pytest.raises(ValueError):
+            ex.forward(x, idx, wt, y)
+        t.index = 0
+    assert len(ran) == 1
