@@ -80,7 +80,7 @@ def test_a_layers_renorm_agrees_with_its_rule(B, monkeypatch, layers, rules, fit
         with pytest.raises(ValueError):
             P.MoELayer(64, 64, 8, 2, torch.zeros(64, 8), **kw)
         return
-    assert P.MoELayer(64, 64, 8, 2, torch.zeros(64, 8), **kw).cfg.renorm == rules
+    assert P.MoELayer(64, 64, 8, 2, torch.zeros(64, 8), **kw).cfg.renorm == rules  # (closed at once, by the stand-in)
     del kw["select"]  # without a rule: as asked, True where nothing is
     assert P.MoELayer(64, 64, 8, 2, torch.zeros(64, 8), **kw).cfg.renorm == (layers is not False)
 
@@ -117,7 +117,8 @@ def layer(B, monkeypatch):
     lay = P.MoELayer(64, 64, 8, 2, torch.zeros(64, 8), dense=torch.zeros(1), select=P.SelectRule(8, 2), max_tokens=4)
     lay.asked = []
     monkeypatch.setattr(B, "moe_route_logits", lambda ctx, x, T, w, out: lay.asked.append((T, tuple(out.shape))))
-    return lay
+    yield lay
+    lay.close()  # (while its context is one that nobody made)
 
 
 def test_rows_whose_logits_are_asked_for_have_the_layers_width_and_type(layer):
