@@ -243,7 +243,7 @@ int moe_route(moe_ctx* ctx, const void* x, int32_t T, const moe_weights* w, int3
 int moe_route_logits(moe_ctx* ctx, const void* x, int32_t T, const moe_weights* w, float* logits, void* stream) {
   if (!ctx || T < 0) return MOE_ERR_INVALID_ARG;
   if (T == 0) return MOE_OK;
-  if (!x || !logits || misaligned(x)) return MOE_ERR_INVALID_ARG;
+  if (!x || !logits || misaligned(x) || ((uintptr_t)logits & 3u)) return MOE_ERR_INVALID_ARG;
   int rc = check_weights(ctx->cfg, w, true, false);
   if (rc != MOE_OK) return rc;
   return launch_route(ctx, x, T, w, nullptr, nullptr, logits, (cudaStream_t)stream);

@@ -393,7 +393,7 @@ int moe_fp4_quantize_rows(const void* src, int32_t dtype, int64_t src_rows, int6
   if (!row_of && rows > src_rows) return MOE_ERR_INVALID_ARG;
   if (rows == 0) return MOE_OK;
   if (!codes || !scales || misaligned(codes) || misaligned(scales) || (src_rows > 0 && !src)) return MOE_ERR_INVALID_ARG;
-  if ((uintptr_t)src % (dtype == MOE_F32 ? 4 : 2)) return MOE_ERR_INVALID_ARG;
+  if ((uintptr_t)src % (dtype == MOE_F32 ? 4 : 2) || ((uintptr_t)row_of & 3u)) return MOE_ERR_INVALID_ARG;
   return launch_fp4_quantize(Fp4Source{src, dtype, row_stride, col_stride, src_rows, row_of, row_div}, rows, n, codes, scales,
                              fp4_shape(rows, n).rp, -1, (cudaStream_t)stream);
 }
@@ -427,7 +427,7 @@ int moe_fp4_pack_dense(int32_t d_model, int32_t d_ff, int32_t n_experts, const v
   const long long fb = (d_ff + 31) / 32, d = d_model, f = d_ff;
   if (gu->n != d_model || gu->rows != n_experts * fb * 64 || down->n != d_ff || down->rows != n_experts * d) return MOE_ERR_INVALID_ARG;
   if (!gu->codes || !gu->scales || !down->codes || !down->scales || misaligned(gu->codes) || misaligned(gu->scales) ||
-      misaligned(down->codes) || misaligned(down->scales))
+      misaligned(down->codes) || misaligned(down->scales) || (((uintptr_t)w_gate | (uintptr_t)w_up | (uintptr_t)w_down) & 1u))
     return MOE_ERR_INVALID_ARG;
   cudaStream_t s = (cudaStream_t)stream;
   size_t cb, sb;

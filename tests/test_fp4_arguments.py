@@ -155,3 +155,17 @@ def test_experts_outputs_lie_on_the_current_device(B, monkeypatch):
             ex.forward(x, idx, wt, y)
         t.index = 0
     assert len(ran) == 1
+
+
+def test_addresses_that_kernels_could_not_read():
+    """Nothing is launched, so no device is needed (the addresses are never followed)."""
+    import ctypes as C
+
+    from paper_2503_00245_b200 import binding as B
+    A = 1 << 20
+    quantize, pack = B._lib().moe_fp4_quantize_rows, B._lib().moe_fp4_pack_dense
+    for off in (1, 2, 3):
+        assert quantize(A, 1, 4, 64, 1, A + off, 1, 4, 64, A, A, None) == 1
+    gu, down = B.moe_fp4(A, A, 256, 64), B.moe_fp4(A, A, 128, 40)
+    for g, u, d in ((A + 1, A, A), (A, A + 1, A), (A, A, A + 1)):
+        assert pack(64, 40, 2, g, u, d, C.addressof(gu), C.addressof(down), None) == 1

@@ -82,3 +82,18 @@ def test_as_many_tokens_as_a_call_can_name():
     assert abs(float(w[T - 1]) - 1 / (1 + np.exp(-1.0))) < RTOL
     del l, idx, w, part
     torch.cuda.empty_cache()
+
+
+def test_logits_that_kernels_could_not_write():
+    from paper_2503_00245_b200 import binding as B
+    x, wr, out = torch.zeros(3, 64, dtype=torch.bfloat16).cuda(), torch.zeros(64, 8, dtype=torch.bfloat16).cuda(), torch.full((32,), 7.0).cuda()
+    ctx = B.moe_create(B.make_config(64, 64, 8, 2))
+    for off in (1, 2, 3):
+        with pytest.raises(B.MoeError) as e:
+            B.moe_route_logits(ctx, x, 3, B.make_weights(wr), out.data_ptr() + off)
+        assert e.value.status == 1
+    torch.cuda.synchronize()
+    assert (out == 7).all()
+    B.moe_route_logits(ctx, x, 3, B.make_weights(wr), out.data_ptr() + 4)
+    assert not out[1:25].any() and out[0] == 7 and (out[25:] == 7).all()
+    B.moe_destroy(ctx)
