@@ -145,6 +145,13 @@ def _strided(t) -> int:
     return t.data_ptr()
 
 
+def _i32(v: int) -> int:
+    """A number that the library takes in 32 bits (of a longer one ctypes would pass the low ones)."""
+    if not -0x80000000 <= v <= 0x7fffffff:
+        raise OverflowError(f"{v} does not fit into 32 bits")
+    return v
+
+
 def _stream(stream=None) -> int:
     if stream is None:
         return _current_raw_stream(_current_device())
@@ -343,7 +350,7 @@ def make_select_config(n_experts, top_k, scoring=MOE_SCORE_SOFTMAX, n_groups=1, 
 
 
 def make_fp4(codes, scales, rows, n) -> moe_fp4:
-    m = moe_fp4(_ptr(codes), _ptr(scales), rows, n)
+    m = moe_fp4(_ptr(codes), _ptr(scales), rows, _i32(n))
     m._keep = (codes, scales)
     return m
 
@@ -359,28 +366,28 @@ def _dtype(t) -> int:
 
 
 def moe_route_logits(ctx, x, T, w: moe_weights, logits, stream=None):
-    _ok(_lib().moe_route_logits(ctx, _ptr(x), T, C.byref(w), _ptr(logits), _stream(stream)), "moe_route_logits")
+    _ok(_lib().moe_route_logits(ctx, _ptr(x), _i32(T), C.byref(w), _ptr(logits), _stream(stream)), "moe_route_logits")
 
 
 def moe_select(cfg: moe_select_config, logits, T, bias, topk_idx, topk_w, stride=None, stream=None):
     """logits: rows `stride` values apart (n_experts by default), each contiguous."""
-    rc = _lib().moe_select(C.addressof(cfg), _strided(logits), _dtype(logits), cfg.n_experts if stride is None else stride, T,
-                           None if bias is None else _ptr(bias), _ptr(topk_idx), _ptr(topk_w), _stream(stream))
+    rc = _lib().moe_select(C.addressof(cfg), _strided(logits), _dtype(logits), cfg.n_experts if stride is None else stride,
+                           _i32(T), None if bias is None else _ptr(bias), _ptr(topk_idx), _ptr(topk_w), _stream(stream))
     if rc:
         raise MoeError(rc, "moe_select")
 
 
 def moe_fp4_bytes(rows: int, n: int):
     a, b = C.c_size_t(), C.c_size_t()
-    _ok(_lib().moe_fp4_bytes(rows, n, C.byref(a), C.byref(b)), "moe_fp4_bytes")
+    _ok(_lib().moe_fp4_bytes(rows, _i32(n), C.byref(a), C.byref(b)), "moe_fp4_bytes")
     return a.value, b.value
 
 
 def moe_fp4_quantize_rows(src, row_of, row_div, rows, codes, scales, stream=None):
     """src [src_rows][n], any strides that are not negative."""
     rc = _lib().moe_fp4_quantize_rows(_strided(src), _dtype(src), src.shape[0], src.stride(0), src.stride(1),
-                                      None if row_of is None else _ptr(row_of), row_div, rows, src.shape[1], _ptr(codes), _ptr(scales),
-                                      _stream(stream))
+                                      None if row_of is None else _ptr(row_of), _i32(row_div), rows, _i32(src.shape[1]), _ptr(codes),
+                                      _ptr(scales), _stream(stream))
     if rc:
         raise MoeError(rc, "moe_fp4_quantize_rows")
 
@@ -393,12 +400,12 @@ def moe_fp4_dequantize_rows(m: moe_fp4, dst, row_stride=None, stream=None):
 
 
 def moe_fp4_pack_dense(d, f, n_experts, w_gate, w_up, w_down, gu: moe_fp4, down: moe_fp4, stream=None):
-    _ok(_lib().moe_fp4_pack_dense(d, f, n_experts, _ptr(w_gate), _ptr(w_up), _ptr(w_down), C.addressof(gu), C.addressof(down),
+    _ok(_lib().moe_fp4_pack_dense(_i32(d), _i32(f), _i32(n_experts), _ptr(w_gate), _ptr(w_up), _ptr(w_down), C.addressof(gu), C.addressof(down),
                                   _stream(stream)), "moe_fp4_pack_dense")
 
 
 def moe_fp4_product(ctx, a: moe_fp4, w: moe_fp4, expert_offsets, n_experts, out, out_stride=None, stream=None):
-    rc = _lib().moe_fp4_product(ctx, C.addressof(a), C.addressof(w), _ptr(expert_offsets), n_experts, _strided(out), _dtype(out),
+    rc = _lib().moe_fp4_product(ctx, C.addressof(a), C.addressof(w), _ptr(expert_offsets), _i32(n_experts), _strided(out), _dtype(out),
                                 w.rows // n_experts if out_stride is None else out_stride, _stream(stream))
     if rc:
         raise MoeError(rc, "moe_fp4_product")
@@ -406,12 +413,12 @@ def moe_fp4_product(ctx, a: moe_fp4, w: moe_fp4, expert_offsets, n_experts, out,
 
 def moe_fp4_workspace_bytes(cfg: moe_config, T: int) -> int:
     n = C.c_size_t()
-    _ok(_lib().moe_fp4_workspace_bytes(C.byref(cfg), T, C.byref(n)), "moe_fp4_workspace_bytes")
+    _ok(_lib().moe_fp4_workspace_bytes(C.byref(cfg), _i32(T), C.byref(n)), "moe_fp4_workspace_bytes")
     return n.value
 
 
 def moe_fp4_experts(ctx, x, T, gu: moe_fp4, down: moe_fp4, topk_idx, topk_w, y, ws, stream=None):
-    rc = _lib().moe_fp4_experts(ctx, _ptr(x), T, C.addressof(gu), C.addressof(down), _ptr(topk_idx), _ptr(topk_w), _ptr(y), _ptr(ws),
+    rc = _lib().moe_fp4_experts(ctx, _ptr(x), _i32(T), C.addressof(gu), C.addressof(down), _ptr(topk_idx), _ptr(topk_w), _ptr(y), _ptr(ws),
                                 ws.nbytes, _stream(stream))
     if rc:
         raise MoeError(rc, "moe_fp4_experts")

@@ -52,7 +52,7 @@ class Fp4Rows:
 
     @classmethod
     def empty(cls, rows, n, device="cuda"):
-        return cls._over(torch.empty(cls._bytes(rows, n), dtype=torch.uint8, device=device), rows, n)
+        return cls._over(torch.empty(cls._bytes(rows, B._i32(n)), dtype=torch.uint8, device=device), rows, n)
 
     @staticmethod
     def _bytes(rows, n):

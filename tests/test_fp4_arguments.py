@@ -169,3 +169,29 @@ def test_addresses_that_kernels_could_not_read():
     gu, down = B.moe_fp4(A, A, 256, 64), B.moe_fp4(A, A, 128, 40)
     for g, u, d in ((A + 1, A, A), (A, A + 1, A), (A, A, A + 1)):
         assert pack(64, 40, 2, g, u, d, C.addressof(gu), C.addressof(down), None) == 1
+
+
+def test_numbers_longer_than_32_bits(B):
+    """Of 2^32 + 5 tokens the library would be told 5."""
+    import paper_2503_00245_b200 as P
+
+    class Rows:  # stands in for a matrix on the device
+        is_cuda, dtype, shape = True, torch.bfloat16, (1, (1 << 32) + 64)
+
+        def data_ptr(self):
+            return 1 << 20
+
+        def stride(self, i):
+            return 1
+
+    A, long, rows = 1 << 20, (1 << 32) + 8, Rows()
+    m, cfg = B.moe_fp4(A, A, 8, 64), B.make_config(64, 64, 8, 2)
+    for v in (long, 1 << 31, -(1 << 31) - 1):
+        for call in (lambda: B.moe_select(B.make_select_config(8, 2), rows, v, None, A, A), lambda: B.moe_route_logits(A, A, v, B.moe_weights(), A),
+                     lambda: B.moe_fp4_bytes(8, v), lambda: B.moe_fp4_quantize_rows(rows, None, 1, 1, A, A),
+                     lambda: B.moe_fp4_quantize_rows(rows, None, v, 1, A, A), lambda: B.moe_fp4_product(A, m, m, A, v, rows, 8),
+                     lambda: B.moe_fp4_workspace_bytes(cfg, v), lambda: B.moe_fp4_experts(A, A, v, m, m, A, A, A, torch.zeros(8)),
+                     lambda: B.moe_fp4_pack_dense(v, 8, 1, A, A, A, m, m), lambda: B.moe_fp4_pack_dense(8, v, 1, A, A, A, m, m),
+                     lambda: B.make_fp4(A, A, 8, v), lambda: P.Fp4Rows.empty(0, v, "cpu")):
+            with pytest.raises(OverflowError):
+                call()
