@@ -212,7 +212,8 @@ int moe_fp4_product(moe_ctx* ctx, const moe_fp4* a, const moe_fp4* w, const int3
                     int32_t out_dtype, int64_t out_stride, void* stream);
 /* The experts' FFN for a given routing (topk_idx, topk_w dev [T][k], e.g. moe_select's), the experts in MXFP4 (moe_fp4_pack_dense):
  *    y[t] = sum_j topk_w[t][j] o_tj,   o = h' W_d,  h = silu(x' W_g) * (x' W_u),   x' and h' = x and h rounded to MXFP4
- * with fp32 sums, h formed in fp32, o in fp32, one rounding of y to cfg.x_dtype.  (h' of a value next to the border between two
+ * with fp32 sums, h formed in fp32, o in fp32, one rounding of y to cfg.x_dtype.  Four bits on both sides of both products: with normal
+ * rows and weights y differs from the unquantised experts' by 0.30 of its RMS.  (h' of a value next to the border between two
  * codes may fall to either side, as the order of the sums has it.)  x, y dev [T][d].  ctx: of moe_create with wd_rank 0 (path and
  * renorm are not looked at); an expert index outside [0, E) is reported by moe_check and the output of its token undefined.
  * ws: moe_fp4_workspace_bytes(cfg, T), enough for fewer tokens too.  Like every call on a ctx, one stream at a time.    */

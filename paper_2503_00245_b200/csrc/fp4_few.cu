@@ -3,9 +3,11 @@
 //
 // What bounds it is latency in front of and behind the stream of bytes, and HBM between.  A CTA (one per SM) belongs to one expert and
 // takes blocks of 64 of its rows, 512 values at a time ("stage": two swizzled tiles of 64 x 128 bytes and their words of scales, three
-// copies), through a ring of five stages or more: 13 MB under way on 148 SMs, twice what the latency of HBM needs.  The ring takes half
-// of an SM's shared memory, so that the down product's CTAs start beside the gate and up product's and have their first stages in
-// place when the hidden rows are (21 us against 20 a layer with all of it and no company).  The rows are the M side of tcgen05.mma
+// copies), through a ring of four stages or more, beside the tokens' codes.  Both fit into half of an SM's shared memory up to 8 tokens
+// at K = 5632 (four stages: 10 MB under way on 148 SMs) and 16 at K = 2048 (four; five up to 8 tokens), so that the down product's
+// CTAs start beside the gate and up product's and have their first stages in place when the hidden rows are: 20 us a layer (one
+// token, d 2048, f 5632), 21 where each CTA takes all of an SM and none starts early.  Longer rows of more tokens take all of it
+// (8 tokens 41 us, 9 tokens 51).  The rows are the M side of tcgen05.mma
 // kind::mxf4 (M = 128: the lower half of an instruction's rows is whatever lies behind the block and is not looked at; an instruction
 // costs its operands' 4 KB of shared-memory reads either way), the tokens N = 16 or 32 columns, whose codes are laid out in shared
 // memory, swizzled.  Both operands' scales go from shared to tensor memory beside the MMAs (two sets of four warps, a stage each in
@@ -15,8 +17,8 @@
 //   warps 2-9    scales                     warps 12-13  epilogue (TMEM lanes 0-31 and 32-63)
 // Most of this code runs once or twice a launch, so it is short rather than unrolled: fetching instructions that were never run costs
 // more than running them (an epilogue unrolled over the tokens: 2 us a block with one token).
-// (The same products on mma.sync, codes widened to E4M3 in registers: 25 us a layer for one token at d 2048, f 5632, two experts;
-// without its MMAs, whose legacy form is slow here, 19; without any arithmetic 14.)
+// (The same products on mma.sync, tiles through the same ring, codes widened to E4M3 in registers: 25 us a layer for one token at d 2048,
+// f 5632, two experts; without its MMAs, whose legacy form is slow here, 19; without any arithmetic 14.)
 //
 // Modes: HIDDEN  gate and up rows -> silu(g) u -> rows of MXFP4 for the next product
 //        OUT     rows of fp32 or bf16

@@ -69,13 +69,13 @@ __device__ __forceinline__ void route_partial(const XT* __restrict__ xr, const u
   }
 }
 
-// Many tokens: one warp per token, lanes split the d axis.
 // A launch without topk_idx leaves the logits themselves in `probs`.
 __device__ __forceinline__ void store_logits(float l0, float l1, int E, int lane, float* out) {
   if (lane < E) out[lane] = l0;
   if (lane + 32 < E) out[lane + 32] = l1;
 }
 
+// Many tokens: one warp per token, lanes split the d axis.
 template <typename XT, int EMAX>
 __global__ void __launch_bounds__(kRouteWarps * 32)
     route_kernel(const XT* __restrict__ x, const uint16_t* __restrict__ w_router, const float* __restrict__ bias, int T,

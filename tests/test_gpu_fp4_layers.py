@@ -1,4 +1,4 @@
-"""4-bit experts at the large widths, and layers whose experts a rule selects, against the checkers.
+"""4-bit experts at the large widths, and layers whose experts a rule selects, against the oracles.
 
 Tolerances: 4-bit experts as tests/test_gpu_fp4.py derives them.  Dense and decomposed experts (the layer's bar, tests/gpu_util.py, is a
 share of the RMS of all outputs; here tokens differ in scale, where weights are not rescaled, so each is held against its own): half a
@@ -44,13 +44,13 @@ def test_experts_at_the_large_widths(large, T):
     ex = P().Fp4Experts(d, f, E, k, gu, down, max_tokens=T)
     y = ex.forward(x, idx, wt)
     assert ex.check() == 0
-    some = torch.randperm(T, generator=torch.Generator().manual_seed(1))[:40].cuda()  # (the checker takes its time)
+    some = torch.randperm(T, generator=torch.Generator().manual_seed(1))[:40].cuda()  # (the oracle takes its time)
     # (telling: the bound, in which all errors have one sign, grows with the contractions: a fifth of the values at the paper's widths, three
     # tenths at 1.45 times those)
     check_experts(y[some], x[some], gu, down, E, d, f, idx[some], wt[some], telling=False)
 
 
-def by_checker(host, k, idx, w):
+def by_oracle(host, k, idx, w):
     """The experts' sum for a given routing, in 64 bits."""
     E = host["w_router"].shape[1]
     _, offsets, perm, inv = O.permute(idx, E)
@@ -82,7 +82,7 @@ def test_layers_with_a_selection_rule(shape, rule, T):
     want = {n: rule[n] for n in ("scoring", "groups", "group_top", "renorm", "scale") if n in rule}
     i64, w64 = Q.select(to64(lay.logits(t["x"])), k, bias=bias.double().cpu().numpy(), kept=rule.get("groups_kept", 1), **want)
     assert np.array_equal(idx.cpu().numpy(), i64) and np.allclose(w.cpu().numpy(), w64, rtol=2.0 ** -20, atol=0)
-    sum64 = by_checker(host, k, i64, w64)
+    sum64 = by_oracle(host, k, i64, w64)
     step = np.exp2(np.floor(np.log2(np.maximum(np.abs(sum64), 1e-300))) - 8) if y.dtype == torch.bfloat16 else 0.0
     excess = (np.abs(to64(y) - sum64) - step) / np.sqrt(np.mean(sum64 ** 2, axis=1, keepdims=True))
     assert excess.max() <= (2e-2 if y.dtype == torch.float32 and T > 16 else 1e-2), excess.max()
