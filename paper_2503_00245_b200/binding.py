@@ -358,11 +358,15 @@ def make_fp4(codes, scales, rows, n) -> moe_fp4:
 _DTYPES = {torch.float32: MOE_F32, torch.bfloat16: MOE_BF16}
 
 
-def _dtype(t) -> int:
-    d = _DTYPES.get(t.dtype)
+def dtype_of(dtype: torch.dtype) -> int:
+    d = _DTYPES.get(dtype)
     if d is None:
-        raise TypeError(f"float32 or bfloat16, not {t.dtype}")
+        raise TypeError(f"float32 or bfloat16, not {dtype}")
     return d
+
+
+def _dtype(t) -> int:
+    return dtype_of(t.dtype)
 
 
 def moe_route_logits(ctx, x, T, w: moe_weights, logits, stream=None):

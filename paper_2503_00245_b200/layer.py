@@ -206,7 +206,7 @@ class Fp4Experts:
     def __init__(self, d_model, d_ff, n_experts, top_k, gu: Fp4Rows, down: Fp4Rows, x_dtype=torch.bfloat16, max_tokens=1, ctx=None):
         self.d, self.k, self.x_dtype, self.max_tokens = d_model, top_k, x_dtype, max_tokens
         self.gu, self.down, self.device = gu, down, gu.device
-        self.cfg = B.make_config(d_model, d_ff, n_experts, top_k, 0, B.MOE_F32 if x_dtype == torch.float32 else B.MOE_BF16)
+        self.cfg = B.make_config(d_model, d_ff, n_experts, top_k, 0, B.dtype_of(x_dtype))
         self.ctx, self.lent = ctx, ctx is not None  # (a layer lends its own)
         _here(gu._tensor, down._tensor)
         if ctx is None:
@@ -277,7 +277,7 @@ class MoELayer:
         self._cuda_index = self.device.index if self.device.type == "cuda" else None
         self.rank = 0 if wd is None else wd[0].shape[1]
         self.cfg = B.make_config(d_model, d_ff, n_experts, top_k, self.rank,
-                                 B.MOE_F32 if x_dtype == torch.float32 else B.MOE_BF16, int(renorm), path)
+                                 B.dtype_of(x_dtype), int(renorm), path)
         if dense is not None:
             self.weights = B.make_weights(w_router, b_router, gud=dense, expert_slot=expert_slot)
         elif wd is not None:
@@ -410,7 +410,7 @@ class OffloadedStack:
         self.fp8 = fp8
         self.d, self.f, self.E, self.k, self.slots = d_model, d_ff, n_experts, top_k, slots
         self.cfg = B.make_config(d_model, d_ff, n_experts, top_k, 0,
-                                 B.MOE_F32 if x_dtype == torch.float32 else B.MOE_BF16, 1, B.MOE_PATH_STREAM)
+                                 B.dtype_of(x_dtype), 1, B.MOE_PATH_STREAM)
         self.slot_bytes = d_ff * 3 * d_model * 2
         self.host, self.routers_t = [], []
         ptrs = []

@@ -195,3 +195,23 @@ def test_numbers_longer_than_32_bits(B):
                      lambda: B.make_fp4(A, A, 8, v), lambda: P.Fp4Rows.empty(0, v, "cpu")):
             with pytest.raises(OverflowError):
                 call()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float64, torch.int16])
+def test_rows_are_of_a_type_that_the_kernels_read(B, monkeypatch, dtype):
+    """(Everything but float32 was read as bfloat16.)"""
+    import paper_2503_00245_b200 as P
+    monkeypatch.setattr(P.layer, "_here", lambda *t: None)
+    monkeypatch.setattr(B, "make_weights", lambda *a, **k: None)
+    monkeypatch.setattr(B, "moe_create", lambda cfg: None)
+    monkeypatch.setattr(B, "moe_workspace_bytes", lambda cfg, T: 16)
+    monkeypatch.setattr(B, "moe_fp4_workspace_bytes", lambda cfg, T: 16)
+    q = P.Fp4Rows.empty(8, 64, "cpu")
+    for ok in (torch.float32, torch.bfloat16):
+        assert P.Fp4Experts(64, 64, 8, 2, q, q, x_dtype=ok).cfg.x_dtype == B.dtype_of(ok)
+        assert P.MoELayer(64, 64, 8, 2, torch.zeros(64, 8), fp4=(q, q), x_dtype=ok).cfg.x_dtype == B.dtype_of(ok)
+    with pytest.raises(TypeError):
+        P.Fp4Experts(64, 64, 8, 2, q, q, x_dtype=dtype)
+    for kind in (dict(dense=torch.zeros(1)), dict(fp4=(q, q))):
+        with pytest.raises(TypeError):
+            P.MoELayer(64, 64, 8, 2, torch.zeros(64, 8), **kind, x_dtype=dtype)
