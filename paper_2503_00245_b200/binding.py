@@ -404,8 +404,8 @@ def moe_fp4_dequantize_rows(m: moe_fp4, dst, row_stride=None, stream=None):
 
 
 def moe_fp4_pack_dense(d, f, n_experts, w_gate, w_up, w_down, gu: moe_fp4, down: moe_fp4, stream=None):
-    _ok(_lib().moe_fp4_pack_dense(_i32(d), _i32(f), _i32(n_experts), _ptr(w_gate), _ptr(w_up), _ptr(w_down), C.addressof(gu), C.addressof(down),
-                                  _stream(stream)), "moe_fp4_pack_dense")
+    _ok(_lib().moe_fp4_pack_dense(_i32(d), _i32(f), _i32(n_experts), _ptr(w_gate), _ptr(w_up), _ptr(w_down), C.addressof(gu),
+                                  C.addressof(down), _stream(stream)), "moe_fp4_pack_dense")
 
 
 def moe_fp4_product(ctx, a: moe_fp4, w: moe_fp4, expert_offsets, n_experts, out, out_stride=None, stream=None):

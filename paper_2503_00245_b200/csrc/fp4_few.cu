@@ -7,10 +7,10 @@
 // at K = 5632 (four stages: 10 MB under way on 148 SMs) and 16 at K = 2048 (four; five up to 8 tokens), so that the down product's
 // CTAs start beside the gate and up product's and have their first stages in place when the hidden rows are: 20 us a layer (one
 // token, d 2048, f 5632), 21 where each CTA takes all of an SM and none starts early.  Longer rows of more tokens take all of it
-// (8 tokens 41 us, 9 tokens 51).  The rows are the M side of tcgen05.mma
-// kind::mxf4 (M = 128: the lower half of an instruction's rows is whatever lies behind the block and is not looked at; an instruction
-// costs its operands' 4 KB of shared-memory reads either way), the tokens N = 16 or 32 columns, whose codes are laid out in shared
-// memory, swizzled.  Both operands' scales go from shared to tensor memory beside the MMAs (two sets of four warps, a stage each in
+// (8 tokens 41 us, 9 tokens 51).
+// The rows are the M side of tcgen05.mma kind::mxf4 (M = 128: the lower half of an instruction's rows is whatever lies behind the block
+// and is not looked at; an instruction costs its operands' 4 KB of shared-memory reads either way), the tokens N = 16 or 32 columns,
+// whose codes are laid out in shared memory, swizzled.  Both operands' scales go from shared to tensor memory beside the MMAs (two sets of four warps, a stage each in
 // turn).  One token, d 2048, f 5632, two of eight experts: 20 us a layer; the stream itself runs at 5.5 TB/s.
 //   warp 0       copies (the ring's first fill: a stage for each warp)
 //   warp 1       tensor memory, MMAs

@@ -74,7 +74,8 @@ __device__ __forceinline__ float reciprocal(float v) {
   return r;
 }
 // e^(a - b), a <= b.  The difference is rounded, which would cost the power |a - b| 2^-24 of itself; what it lost (exact: two-sum) is
-// put back, so the power is as good as expf's (within 2.6 2^-24 of itself, measured over its arguments) and one product's.  0 below e^-104, where fp32 ends.
+// put back, so the power is as good as expf's (within 2.6 2^-24 of itself, measured over its arguments) and one product's.  0 below
+// e^-104, where fp32 ends.
 __device__ __forceinline__ float exp_difference(float a, float b) {
   const float d = a - b, minus_b = d - a, lost = (a - (d - minus_b)) - (b + minus_b), e = expf(d);
   return d > -104.f ? fmaf(e, lost, e) : 0.f;
